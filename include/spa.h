@@ -194,6 +194,42 @@ int spa_packed_attention_bwd_static(const spa_params* p, const void* qkv, const 
                                     const int32_t* seg_offsets, int32_t n_seg, void* dqkv,
                                     int32_t* d_status, void* stream);
 
+/* Attention with a learned bias by buckets of relative position: spa_packed_attention_fwd with
+ *   S_ij = scale * q_i . k_j + table[bucket[off(i, j)]][h],
+ *   off(i, j) = (y_i - y_j + rows - 1) * (2 cols - 1) + x_i - x_j + cols - 1,
+ * where packed row i holds the token idx[i] = b*N + n at row y_i = n / cols and column x_i = n % cols of its image's grid
+ * (the idx of spa_select_pack; N must equal rows * cols).  (The backbone that the paper's blocks belong to, Sec. 3.1, has such
+ * a bias in its attentions; the paper does not say how packed tokens are to have it.)
+ *   bucket: int32[(2 rows - 1) * (2 cols - 1)], each in [0, n_buckets): a bucket for every offset, or few for many;
+ *   table: T[n_buckets][H].  An entry of -inf masks its bucket; a row that is left without a key gives zeros, lse = -inf,
+ *   peak = 0 and no gradient.
+ * peak: float[H][capacity] out, the logarithm of the row's largest probability (max_j S_ij - lse_i), for the backward.
+ * A segment must hold tokens of one image (images, or parts of them such as containers), and no token twice: the device records
+ * SPA_ERR_INVALID_ARG in d_status where it does not, and for an idx or a bucket out of range (no access goes out of bounds; the
+ * results are undefined.  A token that is there twice is seen by the backward only).
+ * workspace: spa_rel_workspace_bytes() bytes, 256-byte aligned; forward and backward may share it, calls that may run at the
+ * same time may not. */
+typedef struct spa_rel_bias {
+  int32_t rows, cols;    /* token grid: rows * cols = N                                   */
+  int32_t n_buckets;     /* rows of the table                                             */
+  const int32_t* bucket; /* device, int32[(2 rows - 1) * (2 cols - 1)]                    */
+  const void* table;     /* device, T[n_buckets][H]                                       */
+} spa_rel_bias;
+size_t spa_rel_workspace_bytes(const spa_params* p, const spa_rel_bias* rel);
+int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const int32_t* seg_offsets,
+                                 int32_t n_seg, const int32_t* idx, void* attn_out, float* lse, float* peak, void* workspace,
+                                 int32_t* d_status, void* stream);
+
+/* Gradient of spa_packed_attention_rel_fwd: dqkv as spa_packed_attention_bwd, and
+ *   dtable[b][h] = sum of dS_ij over all pairs of all segments whose bucket is b     (float[n_buckets][H] out).
+ * Bitwise reproducible: dS is summed in integers, as multiples of a power of two that is chosen by a bound on its size; each dS
+ * is rounded by at most 2^-23 of the largest that its 128 query rows can have (fp32 problems: 2^-40 of its head's).  peak (of the
+ * same forward call) makes that bound tight; without it (NULL) every probability counts as one that may be 1.  Where the bound or a row's lse or
+ * D is not finite, the whole head's column of dtable is NaN.  SPA_FLAG_ONE_PASS_BWD has no effect. */
+int spa_packed_attention_rel_bwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const void* attn_out, const float* lse,
+                                 const float* peak, const void* d_attn_out, const int32_t* seg_offsets, int32_t n_seg,
+                                 const int32_t* idx, void* dqkv, float* dtable, void* workspace, int32_t* d_status, void* stream);
+
 /* Output projection on the packed tokens:  z[i][j] = b_o[j] + sum_c W_o[j][c] * a[i][c].
  * a: T[capacity][C]; W_o: T[C][C]; b_o: T[C] or NULL; z: T[capacity][C] out. */
 int spa_packed_proj(const spa_params* p, const void* a, const void* W_o, const void* b_o,
@@ -319,6 +355,43 @@ int spa_layer_norm(const spa_params* p, const void* x, const void* gamma, const 
 int spa_layer_norm_bwd(const spa_params* p, const void* dy, const void* x, const void* gamma, const float* mean,
                        const float* rstd, const void* add, void* dx, float* dgamma, float* dbeta,
                        void* workspace, void* stream);
+
+/* The norms before and after a block, with its gate and residual scale: the result z of a block's branch is normalised, gated,
+ * scaled and added to the residual stream x, and the sum is normalised for the block that follows.
+ *   zh_t = norm(z[z_row[t]]);  y_t = x_t + scale * gate_t * (g_post zh_t + b_post);  n_t = g_pre norm(y_t) + b_pre,
+ * for each of the B*N tokens, over its C channels.  (The paper's block figure is not in its text; the norms behind the
+ * branches are those of the backbones that such blocks are put into.)
+ *   kind       SPA_NORM_LAYER: (v - mean) / sqrt(var + eps); SPA_NORM_RMS: v / sqrt(mean(v^2) + eps).
+ *   gate_kind  NONE: 1; SCORE: Sigmoid(gate[t]), gate float[B*N] (the selection's scores, Eq. 5); IMAGE: gate T[B][C];
+ *              TOKEN: gate T[B*N][C].  The latter two are taken as they are.
+ *   scale, g_post, b_post, g_pre, b_pre: T[C] or NULL (1 and 0).
+ *   z: T[capacity][C] with z_row int32[B*N] (the inv of spa_select_pack: z's row of a token, or negative: y = x), every row named
+ *   by at most one token; or T[B*N][C] with z_row NULL.
+ *   y: T[B*N][C] out, may be x; n: T[B*N][C] out or NULL (no norm behind the sum); stats: float[4][B*N] out, for the backward, or
+ *   NULL (mean and 1/deviation of z's row, zero where there is none, and of y's; means are zero under RMS).
+ * n is taken from y before y is rounded.  C is limited to 1024 16-byte chunks per row (else SPA_ERR_UNSUPPORTED); H is not used. */
+enum { SPA_NORM_LAYER = 0, SPA_NORM_RMS = 1 };
+enum { SPA_GATE_NONE = 0, SPA_GATE_SCORE = 1, SPA_GATE_IMAGE = 2, SPA_GATE_TOKEN = 3 };
+typedef struct spa_sandwich {
+  int32_t kind;      /* SPA_NORM_*                                                        */
+  int32_t gate_kind; /* SPA_GATE_*                                                        */
+  float eps;
+  const void* gate;
+  const void *scale, *g_post, *b_post, *g_pre, *b_pre;
+} spa_sandwich;
+int spa_sandwich_norm(const spa_params* p, const spa_sandwich* s, const void* x, const void* z, const int32_t* z_row, void* y,
+                      void* n, float* stats, void* stream);
+
+/* Backward of spa_sandwich_norm.  dn: gradient of n, dy: gradient of y from elsewhere (the residual stream); one of them may be
+ * NULL.  y, z, z_row, stats: of the forward call (y may be NULL with dn).
+ *   dx: T[B*N][C] out, may be dy; dz: like z, only rows that a token names are written;
+ *   dgate: float[B*N] (SCORE), float[B][C] (IMAGE), T[B*N][C] (TOKEN) out; dscale, dg_post, db_post, dg_pre, db_pre: float[C] out.
+ * dgate and each of the five may be NULL.  Sums run in a fixed order: results are bitwise reproducible.
+ * workspace: spa_sandwich_workspace_bytes() bytes. */
+size_t spa_sandwich_workspace_bytes(const spa_params* p, const spa_sandwich* s);
+int spa_sandwich_norm_bwd(const spa_params* p, const spa_sandwich* s, const void* dn, const void* dy, const void* y, const void* z,
+                          const int32_t* z_row, const float* stats, void* dx, void* dz, void* dgate, float* dscale, float* dg_post,
+                          float* db_post, float* dg_pre, float* db_pre, void* workspace, void* stream);
 
 /* h = gelu(u) = u Phi(u) and du = dh * gelu'(u) over T[B*N][n_cols]; du may alias dh. */
 int spa_gelu(const spa_params* p, const void* u, int32_t n_cols, void* h, void* stream);

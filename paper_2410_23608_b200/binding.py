@@ -24,6 +24,8 @@ SPA_FLAG_RESIDUAL, SPA_FLAG_INPLACE, SPA_FLAG_GATE_SCALE, SPA_FLAG_SIMT_ONLY, SP
 SPA_FLAG_UNFUSED = 32
 SPA_FLAG_ONE_PASS_BWD = 64
 SPA_FLAG_SHORT_WAITS = 128
+SPA_NORM_LAYER, SPA_NORM_RMS = 0, 1
+SPA_GATE_NONE, SPA_GATE_SCORE, SPA_GATE_IMAGE, SPA_GATE_TOKEN = 0, 1, 2, 3
 
 EXPORTS = (
     "spa_workspace_bytes", "spa_gate", "spa_select_pack", "spa_packed_qkv", "spa_packed_attention_fwd",
@@ -36,6 +38,8 @@ EXPORTS = (
     "spa_overlap_create", "spa_overlap_destroy", "spa_block_fwd", "spa_block_bwd", "spa_layer_fwd", "spa_layer_bwd", "spa_layer_workspace_bytes",
     "spa_probe_exp2", "spa_probe_wait_expiry", "spa_probe_mma_issue", "spa_pack_state_bytes", "spa_gate_select_pack_supported",
     "spa_gate_select_pack", "spa_container_max_segments", "spa_container_offsets",
+    "spa_rel_workspace_bytes", "spa_packed_attention_rel_fwd", "spa_packed_attention_rel_bwd",
+    "spa_sandwich_norm", "spa_sandwich_workspace_bytes", "spa_sandwich_norm_bwd",
 )
 
 
@@ -77,6 +81,17 @@ class SpaLayerBuffers(C.Structure):
                     "x", "g1", "be1", "g2", "be2", "W1", "b1", "W2", "b2", "cu_all", "z", "y1", "t", "out", "u", "h", "m1", "r1",
                     "m2", "r2", "d_out", "dh", "dt", "dy1", "dX", "dW1", "db1", "dW2", "db2", "dg1", "dbe1", "dg2", "dbe2",
                     "workspace", "workspace_side")])
+
+
+class SpaRelBias(C.Structure):
+    """spa_rel_bias of include/spa.h, field for field."""
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("n_buckets", C.c_int32), ("bucket", C.c_void_p), ("table", C.c_void_p)]
+
+
+class SpaSandwich(C.Structure):
+    """spa_sandwich of include/spa.h, field for field."""
+    _fields_ = [("kind", C.c_int32), ("gate_kind", C.c_int32), ("eps", C.c_float), ("gate", C.c_void_p), ("scale", C.c_void_p),
+                ("g_post", C.c_void_p), ("b_post", C.c_void_p), ("g_pre", C.c_void_p), ("b_pre", C.c_void_p)]
 
 
 def make_params(B, N, Cc, H, dtype, capacity=None, flags=0, tau=0.0, softmax_scale=0.0) -> SpaParams:
@@ -144,8 +159,16 @@ def lib() -> C.CDLL:
         L.spa_probe_wait_expiry.argtypes = [i32, vp, vp, vp]
         L.spa_probe_mma_issue.argtypes = [i32, i32, vp, vp, vp]
         L.spa_read_status.argtypes = [vp, vp]
+        pr, ps = C.POINTER(SpaRelBias), C.POINTER(SpaSandwich)
+        for name, args in (("spa_rel_workspace_bytes", [pp, pr]), ("spa_sandwich_workspace_bytes", [pp, ps])):
+            getattr(L, name).restype = C.c_size_t
+            getattr(L, name).argtypes = args
+        L.spa_packed_attention_rel_fwd.argtypes = [pp, pr, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.spa_packed_attention_rel_bwd.argtypes = [pp, pr, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.spa_sandwich_norm.argtypes = [pp, ps, vp, vp, vp, vp, vp, vp, vp]
+        L.spa_sandwich_norm_bwd.argtypes = [pp, ps] + [vp] * 16
         for name in EXPORTS:
-            if name not in ("spa_workspace_bytes", "spa_layer_workspace_bytes", "spa_train_workspace_bytes", "spa_pack_state_bytes", "spa_status_string", "spa_last_cuda_error",
+            if name not in ("spa_workspace_bytes", "spa_rel_workspace_bytes", "spa_sandwich_workspace_bytes", "spa_layer_workspace_bytes", "spa_train_workspace_bytes", "spa_pack_state_bytes", "spa_status_string", "spa_last_cuda_error",
                             "spa_launch_count"):
                 getattr(L, name).restype = C.c_int
         L.spa_status_string.restype = C.c_char_p
@@ -256,6 +279,34 @@ def spa_packed_attention_bwd_static(p, qkv, attn_out, lse, d_attn_out, seg_offse
                                                  _stream(stream)), "spa_packed_attention_bwd_static")
 
 
+def rel_bias(rows, cols, bucket, table) -> SpaRelBias:
+    """A spa_rel_bias from the device tensors bucket (int32 [(2 rows - 1) (2 cols - 1)]) and table ([n_buckets, H]), which it keeps."""
+    if bucket.dtype != torch.int32 or bucket.numel() != (2 * rows - 1) * (2 * cols - 1):
+        raise ValueError("bucket: int32, one for each of the (2 rows - 1) (2 cols - 1) offsets")
+    if table.dim() != 2:
+        raise ValueError("table: [n_buckets, H]")
+    r = SpaRelBias(int(rows), int(cols), int(table.shape[0]), _ptr(bucket), _ptr(table))
+    r.tensors = (bucket, table)
+    return r
+
+
+def spa_rel_workspace_bytes(p, rel) -> int:
+    return int(lib().spa_rel_workspace_bytes(C.byref(p), C.byref(rel)))
+
+
+def spa_packed_attention_rel_fwd(p, rel, qkv, seg_offsets, n_seg, idx, attn_out, lse, peak, workspace, d_status=None, stream=None):
+    _check(lib().spa_packed_attention_rel_fwd(C.byref(p), C.byref(rel), _ptr(qkv), _ptr(seg_offsets), int(n_seg), _ptr(idx), _ptr(attn_out),
+                                              _ptr(lse), _ptr(peak), _ptr(workspace), _ptr(d_status), _stream(stream)),
+           "spa_packed_attention_rel_fwd")
+
+
+def spa_packed_attention_rel_bwd(p, rel, qkv, attn_out, lse, peak, d_attn_out, seg_offsets, n_seg, idx, dqkv, dtable, workspace,
+                                 d_status=None, stream=None):
+    _check(lib().spa_packed_attention_rel_bwd(C.byref(p), C.byref(rel), _ptr(qkv), _ptr(attn_out), _ptr(lse), _ptr(peak), _ptr(d_attn_out),
+                                              _ptr(seg_offsets), int(n_seg), _ptr(idx), _ptr(dqkv), _ptr(dtable), _ptr(workspace),
+                                              _ptr(d_status), _stream(stream)), "spa_packed_attention_rel_bwd")
+
+
 def spa_packed_proj(p, a, W_o, b_o, cu_seqlens, z, d_status=None, stream=None):
     _check(lib().spa_packed_proj(C.byref(p), _ptr(a), _ptr(W_o), _ptr(b_o), _ptr(cu_seqlens), _ptr(z),
                                  _ptr(d_status), _stream(stream)), "spa_packed_proj")
@@ -353,6 +404,34 @@ def spa_layer_norm(p, x, gamma, beta, eps, y, mean, rstd, stream=None):
 def spa_layer_norm_bwd(p, dy, x, gamma, mean, rstd, add, dx, dgamma, dbeta, workspace, stream=None):
     _check(lib().spa_layer_norm_bwd(C.byref(p), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(add), _ptr(dx),
                                     _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _stream(stream)), "spa_layer_norm_bwd")
+
+
+_NORM_KINDS = {"layer": SPA_NORM_LAYER, "rms": SPA_NORM_RMS}
+_GATE_KINDS = {"none": SPA_GATE_NONE, "score": SPA_GATE_SCORE, "image": SPA_GATE_IMAGE, "token": SPA_GATE_TOKEN}
+
+
+def sandwich(kind="layer", gate_kind="none", gate=None, scale=None, g_post=None, b_post=None, g_pre=None, b_pre=None, eps=1e-5) -> SpaSandwich:
+    """A spa_sandwich from device tensors (which it keeps) and the names of its kinds ("layer", "rms"; "none", "score", "image", "token")."""
+    tensors = (gate, scale, g_post, b_post, g_pre, b_pre)
+    s = SpaSandwich(_NORM_KINDS.get(kind, kind), _GATE_KINDS.get(gate_kind, gate_kind), float(eps), *(_ptr(t) for t in tensors))
+    s.tensors = tensors
+    return s
+
+
+def spa_sandwich_norm(p, s, x, z, z_row, y, n, stats=None, stream=None):
+    _check(lib().spa_sandwich_norm(C.byref(p), C.byref(s), _ptr(x), _ptr(z), _ptr(z_row), _ptr(y), _ptr(n), _ptr(stats), _stream(stream)),
+           "spa_sandwich_norm")
+
+
+def spa_sandwich_workspace_bytes(p, s) -> int:
+    return int(lib().spa_sandwich_workspace_bytes(C.byref(p), C.byref(s)))
+
+
+def spa_sandwich_norm_bwd(p, s, dn, dy, y, z, z_row, stats, dx, dz, dgate=None, dscale=None, dg_post=None, db_post=None, dg_pre=None,
+                          db_pre=None, workspace=None, stream=None):
+    _check(lib().spa_sandwich_norm_bwd(C.byref(p), C.byref(s), _ptr(dn), _ptr(dy), _ptr(y), _ptr(z), _ptr(z_row), _ptr(stats), _ptr(dx),
+                                       _ptr(dz), _ptr(dgate), _ptr(dscale), _ptr(dg_post), _ptr(db_post), _ptr(dg_pre), _ptr(db_pre),
+                                       _ptr(workspace), _stream(stream)), "spa_sandwich_norm_bwd")
 
 
 def spa_gelu(p, u, n_cols, h, stream=None):

@@ -227,6 +227,46 @@ int spa_packed_attention_bwd(const spa_params* p, const void* qkv, const void* a
                                    (cudaStream_t)stream);
 }
 
+static int check_rel(const spa_params* p, const spa_rel_bias* r) {
+  int rc = check_params(p);
+  if (rc != SPA_OK) return rc;
+  rc = check_heads(p);
+  if (rc != SPA_OK) return rc;
+  SPA_REQUIRE(r != nullptr, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(r->rows > 0 && r->cols > 0 && (long long)r->rows * r->cols == p->N, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(r->n_buckets > 0, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE((long long)r->n_buckets * p->H <= (1LL << 26), SPA_ERR_UNSUPPORTED);
+  return SPA_OK;
+}
+
+size_t spa_rel_workspace_bytes(const spa_params* p, const spa_rel_bias* rel) {
+  return check_rel(p, rel) == SPA_OK ? rel_workspace_bytes(*p, *rel) : 0;
+}
+
+int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const int32_t* seg_offsets,
+                                 int32_t n_seg, const int32_t* idx, void* attn_out, float* lse, float* peak, void* workspace,
+                                 int32_t* d_status, void* stream) {
+  int rc = check_rel(p, rel);
+  if (rc != SPA_OK) return rc;
+  SPA_PTR(rel->bucket); SPA_PTR(rel->table); SPA_PTR(qkv); SPA_PTR(seg_offsets); SPA_PTR(idx); SPA_PTR(attn_out); SPA_PTR(lse);
+  SPA_PTR(peak); SPA_PTR(workspace);
+  SPA_REQUIRE(n_seg >= 0, SPA_ERR_INVALID_ARG);
+  return launch_attention_rel_fwd(*p, *rel, qkv, seg_offsets, n_seg, idx, attn_out, lse, peak, workspace, d_status,
+                                  (cudaStream_t)stream);
+}
+
+int spa_packed_attention_rel_bwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const void* attn_out, const float* lse,
+                                 const float* peak, const void* d_attn_out, const int32_t* seg_offsets, int32_t n_seg,
+                                 const int32_t* idx, void* dqkv, float* dtable, void* workspace, int32_t* d_status, void* stream) {
+  int rc = check_rel(p, rel);
+  if (rc != SPA_OK) return rc;
+  SPA_PTR(rel->bucket); SPA_PTR(rel->table); SPA_PTR(qkv); SPA_PTR(attn_out); SPA_PTR(lse); SPA_OPT_PTR(peak); SPA_PTR(d_attn_out);
+  SPA_PTR(seg_offsets); SPA_PTR(idx); SPA_PTR(dqkv); SPA_PTR(dtable); SPA_PTR(workspace);
+  SPA_REQUIRE(n_seg >= 0, SPA_ERR_INVALID_ARG);
+  return launch_attention_rel_bwd(*p, *rel, qkv, attn_out, lse, peak, d_attn_out, seg_offsets, n_seg, idx, dqkv, dtable, workspace,
+                                  d_status, (cudaStream_t)stream);
+}
+
 int spa_packed_attention_bwd_static(const spa_params* p, const void* qkv, const void* attn_out, const float* lse,
                                     const void* d_attn_out, const int32_t* seg_offsets, int32_t n_seg, void* dqkv,
                                     int32_t* d_status, void* stream) {
@@ -416,6 +456,54 @@ int spa_layer_norm_bwd(const spa_params* p, const void* dy, const void* x, const
   if (mean == nullptr || rstd == nullptr || dgamma == nullptr || dbeta == nullptr || workspace == nullptr)
     return SPA_ERR_INVALID_ARG;
   return launch_layer_norm_bwd(*p, dy, x, gamma, mean, rstd, add, dx, dgamma, dbeta, workspace, (cudaStream_t)stream);
+}
+
+static int check_sandwich(const spa_params* p, const spa_sandwich* s) {
+  int rc = check_params(p);
+  if (rc != SPA_OK) return rc;
+  SPA_REQUIRE(s != nullptr, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(s->kind == SPA_NORM_LAYER || s->kind == SPA_NORM_RMS, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(s->gate_kind >= SPA_GATE_NONE && s->gate_kind <= SPA_GATE_TOKEN, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(s->eps >= 0.f && s->eps <= 3.0e38f, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(sandwich_supported(*p), SPA_ERR_UNSUPPORTED);
+  if (s->gate_kind != SPA_GATE_NONE) SPA_PTR(s->gate);
+  SPA_OPT_PTR(s->scale); SPA_OPT_PTR(s->g_post); SPA_OPT_PTR(s->b_post); SPA_OPT_PTR(s->g_pre); SPA_OPT_PTR(s->b_pre);
+  return SPA_OK;
+}
+
+int spa_sandwich_norm(const spa_params* p, const spa_sandwich* s, const void* x, const void* z, const int32_t* z_row, void* y,
+                      void* n, float* stats, void* stream) {
+  int rc = check_sandwich(p, s);
+  if (rc != SPA_OK) return rc;
+  SPA_PTR(x); SPA_PTR(z); SPA_OPT_PTR(z_row); SPA_PTR(y); SPA_OPT_PTR(n); SPA_OPT_PTR(stats);
+  if (p->B == 0) return SPA_OK;
+  return launch_sandwich(*p, *s, x, z, z_row, y, n, stats, (cudaStream_t)stream);
+}
+
+size_t spa_sandwich_workspace_bytes(const spa_params* p, const spa_sandwich* s) {
+  return check_sandwich(p, s) == SPA_OK ? sandwich_workspace_bytes(*p, *s) : 0;
+}
+
+int spa_sandwich_norm_bwd(const spa_params* p, const spa_sandwich* s, const void* dn, const void* dy, const void* y, const void* z,
+                          const int32_t* z_row, const float* stats, void* dx, void* dz, void* dgate, float* dscale, float* dg_post,
+                          float* db_post, float* dg_pre, float* db_pre, void* workspace, void* stream) {
+  int rc = check_sandwich(p, s);
+  if (rc != SPA_OK) return rc;
+  SPA_OPT_PTR(dn); SPA_OPT_PTR(dy); SPA_OPT_PTR(y); SPA_PTR(z); SPA_OPT_PTR(z_row); SPA_PTR(stats); SPA_PTR(dx); SPA_PTR(dz);
+  SPA_OPT_PTR(dgate); SPA_OPT_PTR(dscale); SPA_OPT_PTR(dg_post); SPA_OPT_PTR(db_post); SPA_OPT_PTR(dg_pre); SPA_OPT_PTR(db_pre);
+  SPA_PTR(workspace);
+  SPA_REQUIRE(dn != nullptr || dy != nullptr, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(dn == nullptr || y != nullptr, SPA_ERR_INVALID_ARG);
+  SPA_REQUIRE(dgate == nullptr || s->gate_kind != SPA_GATE_NONE, SPA_ERR_INVALID_ARG);
+  if (p->B == 0) {  // sums over no rows
+    for (float* g : {dscale, dg_post, db_post, dg_pre, db_pre}) {
+      const cudaError_t e = g == nullptr ? cudaSuccess : cudaMemsetAsync(g, 0, sizeof(float) * p->C, (cudaStream_t)stream);
+      if (e != cudaSuccess) { set_cuda_error(e, "spa_sandwich_norm_bwd"); return SPA_ERR_CUDA; }
+    }
+    return SPA_OK;
+  }
+  return launch_sandwich_bwd(*p, *s, dn, dy, y, z, z_row, stats, dx, dz, dgate, dscale, dg_post, db_post, dg_pre, db_pre, workspace,
+                             (cudaStream_t)stream);
 }
 
 int spa_gelu(const spa_params* p, const void* u, int32_t n_cols, void* h, void* stream) {

@@ -1,0 +1,217 @@
+// Attention with a learned bias by buckets of relative position, around the attention kernels: what comes before them (the table
+// expanded to one value per offset, the tokens' positions, the bounds that the table's gradient is scaled by) and behind them
+// (the gradient from its integer bins).  The backbone that the paper's blocks belong to (Sec. 3.1) has such a bias in every
+// attention; with packed rows it goes by the tokens' places on the grid, which idx keeps.
+#include "attn_rel.cuh"
+#include "spa_tc.cuh"
+
+namespace spa {
+namespace {
+
+constexpr int kPrepThreads = 256;
+
+struct Prep {
+  const void* table;
+  const int32_t *bucket, *idx, *seg;
+  const void *qkv, *dao;  // backward only
+  float* bias;
+  int32_t *pos, *owner, *bad;
+  unsigned long long* acc;
+  float* bound;
+  int n_seg, capacity, B, N, rows, cols, n_buckets, entries, pitch, C, H;
+  float mul;
+};
+
+// kRelBlocks CTAs.  Forward and backward: bias[h][o] = table[bucket[o]][h] * mul, the rows' positions, the check of idx.  Backward:
+// cleared bins, the last row of every token (two rows of one token show behind the attention), and per CTA and head the largest
+// |v|^2 and |dO|^2 of its rows.
+template <typename T, int D, bool kBwd>
+__global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, int32_t* d_status) {
+  pdl_entry();
+  extern __shared__ uint32_t top[];  // [H][2]
+  const int tid = blockIdx.x * kPrepThreads + threadIdx.x, all = gridDim.x * kPrepThreads;
+  const T* table = static_cast<const T*>(a.table);
+  if (kBwd)
+    for (int i = threadIdx.x; i < 2 * a.H; i += kPrepThreads) top[i] = 0u;
+  const int Np = packed_rows(a.seg, a.n_seg, a.capacity);
+  for (int o = tid; o < a.pitch; o += all) {
+    const int b = o < a.entries ? a.bucket[o] : 0;
+    const bool ok = (unsigned)b < (unsigned)a.n_buckets;
+    if (!ok) record_status(d_status, SPA_ERR_INVALID_ARG);
+    for (int h = 0; h < a.H; ++h)
+      a.bias[(long long)h * a.pitch + o] = ok ? to_f32<T>(table[(long long)b * a.H + h]) * a.mul : 0.f;
+  }
+  for (int i = tid; i < a.capacity + 128; i += all) {
+    int p = 0;
+    if (i < Np) {
+      const int t = ld_dep(a.idx + i);
+      if ((unsigned)t < (unsigned)(a.B * a.N)) {
+        const int n = t % a.N;
+        p = n / a.cols * (2 * a.cols - 1) + n % a.cols;
+        if (kBwd) a.owner[t] = i;
+        // a segment holds tokens of one image
+        const int before = i > 0 ? ld_dep(a.idx + i - 1) : t;
+        if (t / a.N != before / a.N && ld_dep(a.seg + find_segment(a.seg, a.n_seg, i)) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
+      } else {
+        record_status(d_status, SPA_ERR_INVALID_ARG);
+      }
+    }
+    a.pos[i] = p;
+  }
+  if constexpr (kBwd) {
+    for (int i = tid; i < a.n_buckets * a.H; i += all) a.acc[i] = 0ull;
+    for (int i = tid; i < a.H; i += all) a.bad[i] = 0;
+    __syncthreads();
+    constexpr int E = Vec16<T>::kElems;
+    auto norm2 = [](const T* p) {
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / E; ++c) {
+        float f[E];
+        Vec16<T>::to_float(*reinterpret_cast<const uint4*>(p + c * E), f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = fmaf(f[e], f[e], s);
+      }
+      return __float_as_uint(s) & 0x7fffffffu;
+    };
+    for (long long i = tid; i < (long long)Np * a.H; i += all) {
+      const int row = (int)(i / a.H), h = (int)(i - (long long)row * a.H);
+      atomicMax(top + 2 * h, norm2(static_cast<const T*>(a.qkv) + (3ll * row + 2) * a.C + h * D));
+      atomicMax(top + 2 * h + 1, norm2(static_cast<const T*>(a.dao) + (long long)row * a.C + h * D));
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.H; i += kPrepThreads) a.bound[(long long)blockIdx.x * 2 * a.H + i] = __uint_as_float(top[i]);
+  }
+}
+
+// dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.
+__global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const int32_t* seg, int n_seg, int capacity, const int32_t* idx,
+                                                         const int32_t* owner, int tokens, float* __restrict__ dtable, int32_t* d_status) {
+  pdl_entry();
+  extern __shared__ float unit[];  // [H] value of a bin's least bit
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int h = warp; h < g.H; h += 8) {
+    const float b = rel_head_bound(g, h);
+    const bool ok = b < __uint_as_float(0x7f800000u) && ld_dep(g.bad + h) == 0;
+    if (lane == 0) unit[h] = ok ? __uint_as_float((uint32_t)(127 - kRelBits + rel_exponent(b)) << 23) : __uint_as_float(0x7fc00000u);
+  }
+  __syncthreads();
+  const int tid = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
+  for (int i = tid; i < g.n_buckets * g.H; i += all) dtable[i] = (float)((double)(long long)g.acc[i] * (double)unit[i % g.H]);
+  const int Np = packed_rows(seg, n_seg, capacity);
+  for (int i = tid; i < Np; i += all) {
+    const int t = ld_dep(idx + i);
+    if ((unsigned)t < (unsigned)tokens && ld_dep(owner + t) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
+  }
+}
+
+size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Layout {
+  size_t pos, bias, acc, bound, bad, owner, delta, end;
+  int entries, pitch, center;
+};
+Layout layout(const spa_params& p, const spa_rel_bias& r) {
+  Layout l;
+  const int W = 2 * r.cols - 1;
+  l.entries = (2 * r.rows - 1) * W;
+  l.pitch = (l.entries + 3) & ~3;
+  l.center = (r.rows - 1) * W + r.cols - 1;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += aligned(bytes); return here; };
+  l.pos = take(((size_t)p.capacity + 128) * 4);
+  l.bias = take((size_t)p.H * l.pitch * 4);
+  l.acc = take((size_t)r.n_buckets * p.H * 8);
+  l.bound = take((size_t)kRelBlocks * p.H * 8);
+  l.bad = take((size_t)p.H * 4);
+  l.owner = take((size_t)p.B * p.N * 4);
+  l.delta = take((size_t)p.H * p.capacity * 4);
+  l.end = at;
+  return l;
+}
+
+int launch_prep(const spa_params& p, const spa_rel_bias& r, const Layout& l, char* ws, const int32_t* seg, int n_seg, const int32_t* idx,
+                const void* qkv, const void* dao, float mul, int32_t* d_status, cudaStream_t st) {
+  Prep a = {};
+  a.table = r.table;
+  a.bucket = r.bucket;
+  a.idx = idx;
+  a.seg = seg;
+  a.qkv = qkv;
+  a.dao = dao;
+  a.bias = (float*)(ws + l.bias);
+  a.pos = (int32_t*)(ws + l.pos);
+  a.owner = (int32_t*)(ws + l.owner);
+  a.bad = (int32_t*)(ws + l.bad);
+  a.acc = (unsigned long long*)(ws + l.acc);
+  a.bound = (float*)(ws + l.bound);
+  a.n_seg = n_seg;
+  a.capacity = p.capacity;
+  a.B = p.B;
+  a.N = p.N;
+  a.rows = r.rows;
+  a.cols = r.cols;
+  a.n_buckets = r.n_buckets;
+  a.entries = l.entries;
+  a.pitch = l.pitch;
+  a.C = p.C;
+  a.H = p.H;
+  a.mul = mul;
+  const size_t smem = dao != nullptr ? (size_t)2 * p.H * sizeof(uint32_t) : 0;
+#define SPA_PREP(T, D)                                                                                                       \
+  do {                                                                                                                       \
+    if (dao != nullptr) launch_pdl(rel_prep_kernel<T, D, true>, kRelBlocks, kPrepThreads, smem, st, a, d_status);            \
+    else launch_pdl(rel_prep_kernel<T, D, false>, kRelBlocks, kPrepThreads, smem, st, a, d_status);                          \
+  } while (0)
+  const int d = p.C / p.H;
+  if (p.dtype == SPA_F32) { if (d == 32) SPA_PREP(float, 32); else SPA_PREP(float, 64); }
+  else if (d == 32) SPA_PREP(__nv_bfloat16, 32);
+  else SPA_PREP(__nv_bfloat16, 64);
+#undef SPA_PREP
+  SPA_CUDA_CHECK_LAUNCH("rel_prep_kernel");
+  return SPA_OK;
+}
+
+RelView view(const Layout& l, char* ws) {
+  return RelView{(const int32_t*)(ws + l.pos), (const float*)(ws + l.bias), l.pitch, l.entries, l.center};
+}
+
+}  // namespace
+
+size_t rel_workspace_bytes(const spa_params& p, const spa_rel_bias& r) { return layout(p, r).end; }
+
+int launch_attention_rel_fwd(const spa_params& p, const spa_rel_bias& r, const void* qkv, const int32_t* seg, int n_seg,
+                             const int32_t* idx, void* ao, float* lse, float* peak, void* workspace, int32_t* d_status, cudaStream_t st) {
+  const Layout l = layout(p, r);
+  char* ws = static_cast<char*>(workspace);
+  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, nullptr, nullptr, 1.f, d_status, st);
+  if (rc != SPA_OK) return rc;
+  return launch_attention_rel_fwd_simt(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, st);
+}
+
+int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const void* qkv, const void* ao, const float* lse,
+                             const float* peak, const void* dao, const int32_t* seg, int n_seg, const int32_t* idx, void* dqkv,
+                             float* dtable, void* workspace, int32_t* d_status, cudaStream_t st) {
+  const Layout l = layout(p, r);
+  char* ws = static_cast<char*>(workspace);
+  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, qkv, dao, 1.f, d_status, st);
+  if (rc != SPA_OK) return rc;
+  RelGrad g = {};
+  g.acc = (unsigned long long*)(ws + l.acc);
+  g.bucket = r.bucket;
+  g.bound = (const float*)(ws + l.bound);
+  g.peak = peak;
+  g.bad = (int32_t*)(ws + l.bad);
+  g.n_buckets = r.n_buckets;
+  g.H = p.H;
+  rc = launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);
+  if (rc != SPA_OK) return rc;
+  const long long work = (long long)r.n_buckets * p.H > p.capacity ? (long long)r.n_buckets * p.H : p.capacity;
+  const int grid = (int)((work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
+  launch_pdl(rel_finish_kernel, grid, 256, (size_t)p.H * sizeof(float), st, g, seg, n_seg, p.capacity, idx,
+             (const int32_t*)(ws + l.owner), p.B * p.N, dtable, d_status);
+  SPA_CUDA_CHECK_LAUNCH("rel_finish_kernel");
+  return SPA_OK;
+}
+
+}  // namespace spa

@@ -1,0 +1,75 @@
+// Attention with a learned bias by relative position: what its kernels share.
+//
+// A token at row y and column x of a rows x cols grid has the position p = y W + x, W = 2 cols - 1, so that the offset between
+// two tokens is one subtraction: off = p_i - p_j + (rows - 1) W + cols - 1, a number below (2 rows - 1) W.  The table of buckets
+// is expanded to one value per head and offset before the attention kernel runs; any two positions give an offset inside it,
+// also those of tokens of different images, so no look-up needs a check.
+//
+// The table's gradient adds dS_ij to the bin of off(i, j).  Bins are integers: dS times a power of two, so that the order in
+// which the CTAs' atomics arrive changes nothing.  The power comes from a bound on |dS| that is known beforehand:
+//   |dS_ij| = P_ij |dO_i . v_j - D_i| <= 2 P_ij |dO_i| max_j |v_j|     (O_i is a mean of the v_j)
+#pragma once
+
+#include "spa_common.cuh"
+
+namespace spa {
+
+struct RelView {          // what the forward and backward kernels read
+  const int32_t* pos;     // [capacity + 128]
+  const float* bias;      // [H][pitch]: the table's value of every offset
+  int pitch, entries, center;
+};
+
+constexpr int kRelBlocks = kNumSMs;  // CTAs of the kernel that prepares a call, each with its own maxima
+struct RelGrad {
+  unsigned long long* acc;  // [n_buckets][H] sums of dS times 2^(kRelBits - exponent of the head's bound)
+  const int32_t* bucket;    // [entries]
+  const float* bound;       // [kRelBlocks][H][2] largest |v_j|^2 and |dO_i|^2
+  const float* peak;        // [H][capacity] log of the row's largest probability, optional
+  int32_t* bad;             // [H] a row's statistics are not finite
+  int n_buckets, H;
+};
+
+// Bits of the head's bound.  A bin has at most one pair per query, 2^20 in all, and the bound is taken up to a power of two.
+constexpr int kRelBits = 40;
+
+// Exponent e of a bound b < 2^e; zero and values too small for the scale's exponent count as the smallest.
+__device__ __forceinline__ int rel_exponent(float b) {
+  const int e = (int)((__float_as_uint(b) >> 23) & 0xffu) - 126;
+  return e < -80 ? -80 : e;
+}
+__device__ __forceinline__ float rel_scale(int e) { return __uint_as_float((uint32_t)(127 + kRelBits - e) << 23); }
+
+// 2 max |dO| max |v| of a head, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.
+__device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h) {
+  const int lane = threadIdx.x & 31;
+  uint32_t v = 0, d = 0;
+#pragma unroll
+  for (int i = 0; i < (kRelBlocks + 31) / 32; ++i) {
+    if (lane + 32 * i < kRelBlocks) {
+      const float2 b = *reinterpret_cast<const float2*>(g.bound + ((long long)(lane + 32 * i) * g.H + h) * 2);
+      v = max(v, __float_as_uint(b.x));
+      d = max(d, __float_as_uint(b.y));
+    }
+  }
+  v = __reduce_max_sync(0xffffffffu, v);
+  d = __reduce_max_sync(0xffffffffu, d);
+  return 2.f * sqrtf(__uint_as_float(v)) * sqrtf(__uint_as_float(d));
+}
+
+// A row whose logarithm of the sum (NaN, +inf) or D is not finite has dS that are not
+__device__ __forceinline__ void rel_check_row(const RelGrad& g, int h, float lse, float D) {
+  if (!(lse < __uint_as_float(0x7f800000u)) || !(fabsf(D) < __uint_as_float(0x7f800000u))) g.bad[h] = 1;
+}
+
+__device__ __forceinline__ void rel_add(const RelView& r, const RelGrad& g, int h, int off, long long v) {
+  const int b = g.bucket[off + r.center];
+  if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)b * g.H + h, (unsigned long long)v);
+}
+
+int launch_attention_rel_fwd_simt(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
+                                  float* lse, float* peak, cudaStream_t st);
+int launch_attention_rel_bwd_simt(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
+                                  const int32_t* seg, int n_seg, const RelView& rel, const RelGrad& grad, void* dqkv, cudaStream_t st);
+
+}  // namespace spa

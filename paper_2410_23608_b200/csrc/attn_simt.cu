@@ -20,6 +20,7 @@
 // 1.16e-6, 8.5e-7, 8.5e-7, gradients 1.24e-6, 9.4e-7, 5.2e-7).
 #include <math_constants.h>
 
+#include "attn_rel.cuh"
 #include "simt_stage.cuh"
 #include "spa_common.cuh"
 
@@ -164,10 +165,11 @@ __device__ __forceinline__ RowSeg tile_segments(RowSeg* seg_s, const int32_t* se
 // ------------------------------------------------------------------------------------ forward
 template <int D, int kGroups> constexpr int kFwdFloats = (kR + kGroups * 2 * kT) * kLd<D> + kGroups * kR * kLdP;  // Q; per group K and V, P
 
-template <typename T, int D, int kGroups>
+// kRel: a learned bias by relative position is added to S (attn_rel.cu).
+template <typename T, int D, int kGroups, bool kRel>
 __global__ void __launch_bounds__(kGroups * kGroup, 4 / kGroups)
 attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, int C,
-                     float scale, T* __restrict__ ao, float* __restrict__ lse) {
+                     float scale, const RelView rel, T* __restrict__ ao, float* __restrict__ lse, float* __restrict__ peak) {
   pdl_entry();
   constexpr int W = D / kTX, kThreads = kGroups * kGroup;
   extern __shared__ __align__(16) float sm[];
@@ -199,12 +201,25 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
   RowSeg mine[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) { m[i] = -CUDART_INF_F; mine[i] = seg_s[ty + kTY * i]; }
+  const float* bias = kRel ? rel.bias + (long long)h * rel.pitch + rel.center : nullptr;
+  int own_pos[4] = {};
+  if constexpr (kRel) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i0 + ty + kTY * i < Np) own_pos[i] = rel.pos[i0 + ty + kTY * i];
+  }
   own_rows_landed<2>(grp < n_tiles);  // Q; K and V of the first tile may be on their way
   for (int t = grp; t < n_tiles; t += kGroups) {
     cp_async_wait<1>();
     group_sync(grp);  // K; V is waited for behind the first product
     const int kv0 = all.lo + t * kT;
     float s[4][4] = {}, alpha[4];
+    int pos[4] = {};
+    if constexpr (kRel) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (kv0 + tx + kTX * j < all.hi) pos[j] = rel.pos[kv0 + tx + kTX * j];
+    }
     dots<D>(s, Qs, Ks, ty, tx);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -212,7 +227,9 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int ja = kv0 + tx + kTX * j;
-        s[i][j] = (ja >= mine[i].lo && ja < mine[i].hi) ? s[i][j] * scale : -CUDART_INF_F;
+        const bool in = ja >= mine[i].lo && ja < mine[i].hi;
+        if constexpr (kRel) s[i][j] = in ? fmaf(s[i][j], scale, bias[own_pos[i] - pos[j]]) : -CUDART_INF_F;
+        else s[i][j] = in ? s[i][j] * scale : -CUDART_INF_F;
         cm = fmaxf(cm, s[i][j]);
       }
       const float m_new = fmaxf(m[i], max16(cm));
@@ -283,16 +300,19 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
 #pragma unroll 1
       for (int k = mine[i].lo; k < mine[i].hi; ++k) {
         const T* key = qkv + k * ld + C + h * D;
-        const float p = expf(row_dot<T, D>(qkv + row * ld + h * D, key) * scale - m[i]);
+        const float b = kRel ? bias[own_pos[i] - rel.pos[k]] : 0.f;
+        const float p = expf(row_dot<T, D>(qkv + row * ld + h * D, key) * scale + b - m[i]);
 #pragma unroll
         for (int d = 0; d < W; ++d) o[i][d] = fmaf(p, to_f32<T>(key[C + tx * W + d]), o[i][d]);
       }
     }
-    const float inv_l = 1.f / l[i];
+    // biases of -inf may leave a row without a key: zeros
+    const float inv_l = kRel && l[i] == 0.f ? 0.f : 1.f / l[i];
 #pragma unroll
     for (int d = 0; d < W; ++d) o[i][d] *= inv_l;
     store_row<T, W>(ao + (long long)row * C + h * D + tx * W, o[i]);
     if (tx == 0) lse[(long long)h * capacity + row] = m[i] + logf(l[i]);
+    if (kRel && tx == 0) peak[(long long)h * capacity + row] = l[i] == 0.f ? 0.f : -logf(l[i]);
   }
 }
 
@@ -303,11 +323,11 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
 // blockIdx.z = 1: own rows are keys, streamed rows queries, everything transposed: dV += P^T dO, dK += dS^T Q.
 template <int D, int kGroups> constexpr int kBwdFloats = (2 * kR + kGroups * 2 * kT) * kLd<D> + kGroups * (kR * kLdP + 2 * kT);
 
-template <typename T, int D, int kGroups>
+template <typename T, int D, int kGroups, bool kRel>
 __global__ void __launch_bounds__(kGroups * kGroup, 4 / kGroups)
 attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
                      const T* dao, const int32_t* seg, int n_seg, int capacity, int C,
-                     float scale, T* __restrict__ dqkv) {
+                     float scale, const RelView rel, const RelGrad grad, T* __restrict__ dqkv) {
   constexpr int kThreads = kGroups * kGroup;
   pdl_entry();
   constexpr int W = D / kTX, E = Vec16<T>::kElems;
@@ -366,6 +386,15 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
   float my_lse[4] = {}, my_D[4] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) mine[i] = seg_s[ty + kTY * i];
+  const float* bias = kRel ? rel.bias + (long long)h * rel.pitch + rel.center : nullptr;
+  int own_pos[4] = {};
+  float table_scale = 0.f;
+  if constexpr (kRel) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i0 + ty + kTY * i < Np) own_pos[i] = rel.pos[i0 + ty + kTY * i];
+    if (dq) table_scale = rel_scale(rel_exponent(rel_head_bound(grad, h)));  // every warp takes it by itself
+  }
   if (dq) {
     // lane tx < 4 fetches row ty + 8 tx, the others take it from there
     const int r = i0 + ty + kTY * (tx & 3);
@@ -375,6 +404,9 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
       my_D[i] = __shfl_sync(0xffffffffu, dv, i, kTX);
       my_lse[i] = __shfl_sync(0xffffffffu, lv, i, kTX);
     }
+    if constexpr (kRel) {
+      if (r < Np) rel_check_row(grad, h, lv, dv);
+    }
   }
   float acc1[4][W] = {}, acc2[4][W] = {};  // dQ | dK and dV
   own_rows_landed<1>(grp < n_tiles);
@@ -383,6 +415,12 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
     group_sync(grp);
     const int y0 = all.lo + t * kT;
     float s[4][4] = {}, dp[4][4] = {};
+    int pos[4] = {};
+    if constexpr (kRel) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (y0 + tx + kTX * j < all.hi) pos[j] = rel.pos[y0 + tx + kTX * j];
+    }
     dots<D>(s, A1, Y1, ty, tx);
     dots<D>(dp, A2, Y2, ty, tx);
 #pragma unroll
@@ -391,9 +429,19 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
       for (int j = 0; j < 4; ++j) {
         const int c = tx + kTX * j, ya = y0 + c;
         const float l = dq ? my_lse[i] : s2[c], Dv = dq ? my_D[i] : s2[kT + c];
-        const float p = (ya >= mine[i].lo && ya < mine[i].hi) ? expf(s[i][j] * scale - l) : 0.f;
-        if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
-        dp[i][j] = p * (dp[i][j] - Dv);
+        const bool in = ya >= mine[i].lo && ya < mine[i].hi;
+        float p;
+        if constexpr (kRel) {
+          const int off = dq ? own_pos[i] - pos[j] : pos[j] - own_pos[i];
+          p = in && l != -CUDART_INF_F ? expf(fmaf(s[i][j], scale, bias[off]) - l) : 0.f;  // no key: no weight
+          if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
+          dp[i][j] = in ? p * (dp[i][j] - Dv) : 0.f;
+          if (dq && in) rel_add(rel, grad, h, off, __float2ll_rn(dp[i][j] * table_scale));
+        } else {
+          p = in ? expf(s[i][j] * scale - l) : 0.f;
+          if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
+          dp[i][j] = p * (dp[i][j] - Dv);
+        }
       }
     const int n = all.hi - y0 < kT ? all.hi - y0 : kT;
     if (!dq) {
@@ -447,7 +495,9 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
       for (int k = mine[i].lo; k < mine[i].hi; ++k) {
         const int q = dq ? row : k, j = dq ? k : row;  // query and key of the pair
         const T *Q = qkv + q * ld + h * D, *K = qkv + j * ld + C + h * D, *dO = dao + (long long)q * C + h * D;
-        const float p = expf(row_dot<T, D>(Q, K) * scale - lse[(long long)h * capacity + q]);
+        const float b = kRel ? bias[dq ? own_pos[i] - rel.pos[k] : rel.pos[k] - own_pos[i]] : 0.f;
+        const float lq = lse[(long long)h * capacity + q];
+        const float p = kRel && lq == -CUDART_INF_F ? 0.f : expf(row_dot<T, D>(Q, K) * scale + b - lq);
         const float ds = p * (row_dot<T, D>(dO, K + C) - row_dot<T, D>(dO, ao + (long long)q * C + h * D));
 #pragma unroll
         for (int d = 0; d < W; ++d) {
@@ -464,30 +514,30 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
   }
 }
 
-template <typename T, int D, int kGroups>
-int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,
-               cudaStream_t st) {
-  auto kern = attn_fwd_simt_kernel<T, D, kGroups>;
+template <typename T, int D, int kGroups, bool kRel>
+int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
+               float* peak, cudaStream_t st) {
+  auto kern = attn_fwd_simt_kernel<T, D, kGroups, kRel>;
   constexpr int kSmem = kFwdFloats<D, kGroups> * (int)sizeof(float);
   static DeviceOnce attr;
   cudaError_t e = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
   if (e != cudaSuccess) { set_cuda_error(e, "attn_fwd_simt_kernel"); return SPA_ERR_CUDA; }
   launch_pdl(kern, dim3((p.capacity + kR - 1) / kR, p.H), kGroups * kGroup, kSmem, st, (const T*)qkv, seg, n_seg, p.capacity, p.C,
-             softmax_scale_of(p), (T*)ao, lse);
+             softmax_scale_of(p), rel, (T*)ao, lse, peak);
   SPA_CUDA_CHECK_LAUNCH("attn_fwd_simt_kernel");
   return SPA_OK;
 }
 
-template <typename T, int D, int kGroups>
+template <typename T, int D, int kGroups, bool kRel>
 int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
-               const int32_t* seg, int n_seg, void* dqkv, cudaStream_t st) {
-  auto kern = attn_bwd_simt_kernel<T, D, kGroups>;
+               const int32_t* seg, int n_seg, const RelView& rel, const RelGrad& grad, void* dqkv, cudaStream_t st) {
+  auto kern = attn_bwd_simt_kernel<T, D, kGroups, kRel>;
   constexpr int kSmem = kBwdFloats<D, kGroups> * (int)sizeof(float);
   static DeviceOnce attr;
   cudaError_t e = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
   if (e != cudaSuccess) { set_cuda_error(e, "attn_bwd_simt_kernel"); return SPA_ERR_CUDA; }
   launch_pdl(kern, dim3((p.capacity + kR - 1) / kR, p.H, 2), kGroups * kGroup, kSmem, st, (const T*)qkv, (const T*)ao, lse,
-             (const T*)dao, seg, n_seg, p.capacity, p.C, softmax_scale_of(p), (T*)dqkv);
+             (const T*)dao, seg, n_seg, p.capacity, p.C, softmax_scale_of(p), rel, grad, (T*)dqkv);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_simt_kernel");
   return SPA_OK;
 }
@@ -508,23 +558,33 @@ bool one_group(const spa_params& p, int n_seg, bool forward) {
 
 }  // namespace
 
-#define SPA_SIMT_LAUNCH(WHICH, FORWARD, ...)                                                                               \
+#define SPA_SIMT_LAUNCH(WHICH, FORWARD, REL, ...)                                                                          \
   const int d = p.C / p.H;                                                                                               \
   if (one_group(p, n_seg, FORWARD)) {                                                                                             \
-    if (p.dtype == SPA_F32) return d == 32 ? WHICH<float, 32, 1>(__VA_ARGS__) : WHICH<float, 64, 1>(__VA_ARGS__);        \
-    return d == 32 ? WHICH<__nv_bfloat16, 32, 1>(__VA_ARGS__) : WHICH<__nv_bfloat16, 64, 1>(__VA_ARGS__);                \
+    if (p.dtype == SPA_F32) return d == 32 ? WHICH<float, 32, 1, REL>(__VA_ARGS__) : WHICH<float, 64, 1, REL>(__VA_ARGS__);        \
+    return d == 32 ? WHICH<__nv_bfloat16, 32, 1, REL>(__VA_ARGS__) : WHICH<__nv_bfloat16, 64, 1, REL>(__VA_ARGS__);                \
   }                                                                                                                      \
-  if (p.dtype == SPA_F32) return d == 32 ? WHICH<float, 32, 2>(__VA_ARGS__) : WHICH<float, 64, 2>(__VA_ARGS__);          \
-  return d == 32 ? WHICH<__nv_bfloat16, 32, 2>(__VA_ARGS__) : WHICH<__nv_bfloat16, 64, 2>(__VA_ARGS__)
+  if (p.dtype == SPA_F32) return d == 32 ? WHICH<float, 32, 2, REL>(__VA_ARGS__) : WHICH<float, 64, 2, REL>(__VA_ARGS__);          \
+  return d == 32 ? WHICH<__nv_bfloat16, 32, 2, REL>(__VA_ARGS__) : WHICH<__nv_bfloat16, 64, 2, REL>(__VA_ARGS__)
 
 int launch_attention_fwd_simt(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao,
                               float* lse, cudaStream_t st) {
-  SPA_SIMT_LAUNCH(fwd_launch, true, p, qkv, seg, n_seg, ao, lse, st);
+  SPA_SIMT_LAUNCH(fwd_launch, true, false, p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, st);
 }
 
 int launch_attention_bwd_simt(const spa_params& p, const void* qkv, const void* ao, const float* lse,
                               const void* dao, const int32_t* seg, int n_seg, void* dqkv, cudaStream_t st) {
-  SPA_SIMT_LAUNCH(bwd_launch, false, p, qkv, ao, lse, dao, seg, n_seg, dqkv, st);
+  SPA_SIMT_LAUNCH(bwd_launch, false, false, p, qkv, ao, lse, dao, seg, n_seg, RelView{}, RelGrad{}, dqkv, st);
+}
+
+int launch_attention_rel_fwd_simt(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
+                                  float* lse, float* peak, cudaStream_t st) {
+  SPA_SIMT_LAUNCH(fwd_launch, true, true, p, qkv, seg, n_seg, rel, ao, lse, peak, st);
+}
+
+int launch_attention_rel_bwd_simt(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
+                                  const int32_t* seg, int n_seg, const RelView& rel, const RelGrad& grad, void* dqkv, cudaStream_t st) {
+  SPA_SIMT_LAUNCH(bwd_launch, false, true, p, qkv, ao, lse, dao, seg, n_seg, rel, grad, dqkv, st);
 }
 #undef SPA_SIMT_LAUNCH
 

@@ -257,6 +257,21 @@ int launch_layer_norm_bwd(const spa_params& p, const void* dy, const void* x, co
                           const float* rstd, const void* add, void* dx, float* dgamma, float* dbeta, void* workspace,
                           cudaStream_t st, const int32_t* dy_row = nullptr, const int32_t* dz_row = nullptr,
                           void* dz = nullptr);
+// the norms around a block (sandwich.cu)
+bool sandwich_supported(const spa_params& p);
+size_t sandwich_workspace_bytes(const spa_params& p, const spa_sandwich& s);
+int launch_sandwich(const spa_params& p, const spa_sandwich& s, const void* x, const void* z, const int32_t* z_row, void* y,
+                    void* n, float* stats, cudaStream_t st);
+int launch_sandwich_bwd(const spa_params& p, const spa_sandwich& s, const void* dn, const void* dy, const void* y, const void* z,
+                        const int32_t* z_row, const float* stats, void* dx, void* dz, void* dgate, float* dscale, float* dg_post,
+                        float* db_post, float* dg_pre, float* db_pre, void* workspace, cudaStream_t st);
+// attention with a bias by relative position (attn_rel.cu)
+size_t rel_workspace_bytes(const spa_params& p, const spa_rel_bias& r);
+int launch_attention_rel_fwd(const spa_params& p, const spa_rel_bias& r, const void* qkv, const int32_t* seg, int n_seg,
+                             const int32_t* idx, void* ao, float* lse, float* peak, void* workspace, int32_t* d_status, cudaStream_t st);
+int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const void* qkv, const void* ao, const float* lse,
+                             const float* peak, const void* dao, const int32_t* seg, int n_seg, const int32_t* idx, void* dqkv,
+                             float* dtable, void* workspace, int32_t* d_status, cudaStream_t st);
 int launch_gelu(const spa_params& p, const void* u, const void* dh, int n_cols, void* out, cudaStream_t st);
 int launch_copy_tokens(const spa_params& p, const void* src, void* dst, cudaStream_t st);  // dst[B*N][C] = src
 
