@@ -9,6 +9,9 @@ namespace spa {
 namespace {
 
 constexpr int kPrepThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f;  // the tensor-core kernels take exponentials in base 2
+
+bool use_tc(const spa_params& p) { return !(p.flags & SPA_FLAG_SIMT_ONLY) && tc_attention_fwd_supported(p); }
 
 struct Prep {
   const void* table;
@@ -184,8 +187,10 @@ int launch_attention_rel_fwd(const spa_params& p, const spa_rel_bias& r, const v
                              const int32_t* idx, void* ao, float* lse, float* peak, void* workspace, int32_t* d_status, cudaStream_t st) {
   const Layout l = layout(p, r);
   char* ws = static_cast<char*>(workspace);
-  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, nullptr, nullptr, 1.f, d_status, st);
+  const bool tc = use_tc(p);
+  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, nullptr, nullptr, tc ? kLog2e : 1.f, d_status, st);
   if (rc != SPA_OK) return rc;
+  if (tc) return launch_attention_rel_fwd_tc(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, d_status, st);
   return launch_attention_rel_fwd_simt(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, st);
 }
 

@@ -67,6 +67,8 @@ __device__ __forceinline__ void rel_add(const RelView& r, const RelGrad& g, int 
   if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)b * g.H + h, (unsigned long long)v);
 }
 
+int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
+                                float* lse, float* peak, int32_t* d_status, cudaStream_t st);
 int launch_attention_rel_fwd_simt(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
                                   float* lse, float* peak, cudaStream_t st);
 int launch_attention_rel_bwd_simt(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,

@@ -19,6 +19,7 @@
 #include <mutex>
 #include <unordered_map>
 
+#include "attn_rel.cuh"
 #include "attn_tc.cuh"
 
 namespace spa {
@@ -47,6 +48,7 @@ __device__ __forceinline__ bool tile_has_long_rows(const int32_t* s_off, const i
 }
 
 constexpr int kFwdSegStage = 2048;
+constexpr int kSegStageRel = 512;  // the tables need the memory
 
 // c[j] of lane 4 i + k becomes c[k] of lane 4 i + j
 __device__ __forceinline__ void transpose_quads(uint4 (&c)[4], int lane) {
@@ -65,17 +67,48 @@ __device__ __forceinline__ void transpose_quads(uint4 (&c)[4], int lane) {
   swap(c[0], c[2], 2);
   swap(c[1], c[3], 2);
 }
-template <int D> struct FwdSmem {
+// Where the bias by relative position is read (attn_rel.cu): nowhere, in shared memory, in global memory
+enum RelTable { kNoRel = 0, kRelShared = 1, kRelGlobal = 2 };
+
+template <int D, int kRel = kNoRel> struct FwdSmem {
   // Q, 2 x K, 2 x V.  Two CTAs stay below 196 KB of an SM: with 228 (a second Q tile) the kernels that run before and after
   // on the same SMs lost 3 to 5 us, the gate and the packing most (128 images of 196 tokens, forward: 88 -> 92 us).
   static constexpr int kTile = HeadTile<D>::kTileBytes;
   static constexpr int kBar = 5 * kTile;                   // 12 barriers, TMEM slot, abort flag, four item slots
   static constexpr int kXch = kBar + 256;                  // row maxima: [2 tile parities][2 halves][128 rows]
   static constexpr int kXl = kXch + 2048;                  // row sums: [2 halves][128 rows]
+  static constexpr int kSegStage = kRel == kNoRel ? kFwdSegStage : kSegStageRel;
   static constexpr int kSeg = kXl + 1024;                  // staged segment offsets
-  static constexpr int kOrder = kSeg + (kFwdSegStage + 4) * 4;
-  static constexpr int kBytes = kOrder + (int)sizeof(ItemOrder) + 1024;  // and the alignment of the base
+  static constexpr int kOrder = kSeg + (kSegStage + 4) * 4;
+  // with a bias: the keys' positions of two tiles, a copy for each quarter's warps, and the tables of two items
+  static constexpr int kPos = kOrder + (int)sizeof(ItemOrder);
+  static constexpr int kTable = kPos + (kRel != kNoRel ? 4 * 2 * kKV * 4 : 0);
+  static constexpr int kBytes = kTable + 1024;  // and the alignment of the base
+  static constexpr int bytes(int pitch) { return kBytes + (kRel == kRelShared ? 2 * pitch * 4 : 0); }
 };
+
+// kN head dimensions from column `col` + `first` on of a row's output from the keys of its segment alone: rare, one key after the
+// other from global memory.
+template <int kN>
+__device__ __noinline__ void rel_row_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, int C, int col, int first, int d, int row, int lo,
+                                           int hi, float scale_log2e, const RelView& rel, int h, float m, float inv_l) {
+  const __nv_bfloat16* q = qkv + (long long)row * 3 * C + col;
+  const float* bias = rel.bias + (long long)h * rel.pitch + rel.center + rel.pos[row];
+  for (int e0 = 0; e0 < kN; e0 += 8) {
+    float acc[8] = {};
+    for (int j = lo; j < hi; ++j) {
+      const __nv_bfloat16 *k = qkv + (long long)j * 3 * C + C + col, *v = k + C + first + e0;
+      float s = 0.f;
+      for (int e = 0; e < d; ++e) s = fmaf(__bfloat162float(q[e]), __bfloat162float(k[e]), s);
+      const float p = ptx::ex2_approx(fmaf(s, scale_log2e, bias[-rel.pos[j]]) - (m == -CUDART_INF_F ? 0.f : m));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, __bfloat162float(v[e]), acc[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= inv_l;
+    *reinterpret_cast<uint4*>(ao + (long long)row * C + col + first + e0) = Vec16<__nv_bfloat16>::from_float(acc);
+  }
+}
 
 // One persistent pipeline per CTA over all tiles of all its items.  Phases are counted over the whole run, nothing is set
 // up per item and no barrier joins the CTA: while the softmax warps finish an item (normalise, store), the next item's Q,
@@ -84,13 +117,17 @@ template <int D> struct FwdSmem {
 // item and static strides an item cost 4 700 to 7 100 clocks outside its loop.  Before and after: 16 segments of 210 to
 // 1 680 rows, 8 heads of 32: 84 -> 67 us; of 64: 74 -> 55; 32 segments of 58 to 518 rows, 12 heads of 64: 40 -> 34;
 // 128 segments of 98 to 196 rows, 12 heads of 64: 54 -> 51; one segment of 98 rows: 6.0 us, as before.
-template <int D>
+//
+// kRel: S gets a bias by relative position, in units of log 2.  A tile's keys come as positions in shared memory; a pair's bias is
+// then one subtraction and one look-up in the head's table, which the issuing warp fetches an item ahead (kRelShared), or in
+// global memory where two tables do not fit.
+template <int D, int kRel>
 __global__ void __launch_bounds__(kFwdThreads, 2)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, int n_seg, int capacity,
-                   int C, int H, float scale_log2e, __nv_bfloat16* __restrict__ ao, float* __restrict__ lse,
-                   unsigned* counter, bool even_items, int32_t* d_status) {
+                   int C, int H, float scale_log2e, const RelView rel, const __nv_bfloat16* qkv, __nv_bfloat16* __restrict__ ao,
+                   float* __restrict__ lse, float* __restrict__ peak, unsigned* counter, bool even_items, int32_t* d_status) {
   using HT = HeadTile<D>;
-  using SM = FwdSmem<D>;
+  using SM = FwdSmem<D, kRel>;
   constexpr int kTile = HT::kTileBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool is_softmax = warp < kSoftmaxThreads / 32;  // warps 0-7; warp 8 issues the copies and the products
@@ -120,6 +157,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   float* xl = reinterpret_cast<float*>(smem_al + SM::kXl);
   int32_t* seg_s = reinterpret_cast<int32_t*>(smem_al + SM::kSeg);
   ItemOrder* order = reinterpret_cast<ItemOrder*>(smem_al + SM::kOrder);
+  auto bar_table = [&](int item) { return bar + 200 + 16 * (item & 1); };  // the table of the item has landed; between the item slots
+  auto table_s = [&](int item) { return smem_base + SM::kTable + (item & 1) * rel.pitch * 4; };
 
   // The thread that sets the barriers up belongs to the warp that later issues the copies counted on them.
   if (tid == kSoftmaxThreads) {
@@ -128,6 +167,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       ptx::mbar_init(bar_item(b), 1);
       ptx::mbar_init(bar_k(b), 1);
       ptx::mbar_init(bar_v(b), 1);
+      if (kRel == kRelShared) ptx::mbar_init(bar_table(b), 1);
     }
     ptx::mbar_init(bar_q, 1);
     ptx::mbar_init(bar_s, 1);
@@ -139,7 +179,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
     ptx::fence_mbar_init();
   }
   pdl_entry();  // everything up to the wait touches no global memory
-  const bool staged = n_seg < kFwdSegStage;
+  const bool staged = n_seg < SM::kSegStage;
   if (staged)
     for (int i = tid; i <= n_seg; i += kFwdThreads) seg_s[i] = ld_dep(seg + i);
   const int Np = packed_rows(seg, n_seg, capacity);
@@ -200,7 +240,19 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
     }
     bool order_ready = false;
     bool more = true;                                     // numbers are drawn until one lies past the last item
+    int tables = 0;                                       // items whose table has been asked for
     auto announce = [&](const Cursor& c) {
+      if constexpr (kRel == kRelShared) {
+        // its memory: the softmax warps are through with the tables of all items that are two behind this one (see bar_sfree)
+        if (c.n_tiles > 0) {
+          if (ptx::elect_one()) {
+            ptx::mbar_expect_tx(bar_table(c.item), rel.pitch * 4);
+            ptx::bulk_load(table_s(c.item), rel.bias + (long long)c.h * rel.pitch, rel.pitch * 4, bar_table(c.item));
+          }
+          tables = c.item + 1;
+        }
+        __syncwarp();
+      }
       if (lane == 0) {
         const uint32_t slot = item_slot(c.item);
         ptx::sts_s32(slot, c.q0);
@@ -362,6 +414,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       for (int i = gv > 2 ? gv - 2 : 0; i < gv; ++i) ptx::mbar_wait(bar_v(i & 1), (i >> 1) & 1);
       for (int i = gk > 2 ? gk - 2 : 0; i < gk; ++i) ptx::mbar_wait(bar_k(i & 1), (i >> 1) & 1);
       if (q_item >= 0) ptx::mbar_wait(bar_q, q_item & 1);
+      if (kRel == kRelShared)
+        for (int i = tables > 2 ? tables - 2 : 0; i < tables; ++i) ptx::mbar_wait(bar_table(i), (i >> 1) & 1);
       while (more && draws && drawn < n_items) drawn = draw_item(counter, given, n_items, own);
     }
     __syncwarp();
@@ -389,7 +443,32 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       int lo = mine.lo - ptx::lds_s32(item_slot(it) + 8) - col0, hi = mine.hi - mine.lo + lo;
       bool first = true;
       float m = -CUDART_INF_F, l = 0.f;  // m: the maximum the stored P and O refer to (may lag the true one by kRescaleGap)
+      // With a bias: this thread's two of the tile's key positions (as distances in the table, in bytes, negative), its row's place
+      // in the table
+      const int* key_pos = nullptr;
+      uint32_t bias_at = 0;
+      const char* bias_g = nullptr;
+      float top = -CUDART_INF_F;
+      const uint32_t pos_q = smem_base + SM::kPos + quarter * 2 * kKV * 4;
+      if constexpr (kRel != kNoRel) {
+        key_pos = rel.pos + ptx::lds_s32(item_slot(it) + 8) + 2 * (half * 32 + lane);
+        const int own = rel.pos[ptx::lds_s32(item_slot(it)) + rl], k0 = key_pos[0], k1 = key_pos[1];
+        ptx::sts_2s32(pos_q + (g & 1) * kKV * 4 + 8 * (half * 32 + lane), -4 * k0, -4 * k1);
+        bias_at = 4 * (rel.center + own);
+        if constexpr (kRel == kRelShared) {
+          bias_at += table_s(it);
+          wait(bar_table(it), (it >> 1) & 1);
+        } else {
+          bias_g = reinterpret_cast<const char*>(rel.bias + (long long)ptx::lds_s32(item_slot(it) + 4) * rel.pitch);
+        }
+        ptx::named_barrier(1 + quarter, 64);
+      }
       for (; left > 0; --left, ++g, lo -= kKV, hi -= kKV) {
+        int k0 = 0, k1 = 0;
+        if constexpr (kRel != kNoRel) {
+          key_pos += kKV;
+          if (left > 1) { k0 = key_pos[0]; k1 = key_pos[1]; }
+        }
         // ---- S_t into registers: TMEM loads in flight together, one wait
         wait(bar_s, g & 1);
         ptx::tc_fence_after_sync();
@@ -404,6 +483,22 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
 #pragma unroll
         for (int c = 0; c < kCols / 32; ++c) {
           need[c] = c * 32 < hi && c * 32 + 32 > lo;
+          if constexpr (kRel != kNoRel) {
+            if (need[c]) {
+              const uint32_t at = pos_q + (g & 1) * kKV * 4 + 4 * (col0 + c * 32);
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) {
+                int k[4];
+                ptx::lds_4s32(at + 4 * j, k);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  const float b = kRel == kRelShared ? ptx::lds_f32(bias_at + k[u])
+                                                     : *reinterpret_cast<const float*>(bias_g + (bias_at + k[u]));
+                  s[c * 32 + j + u] = __float_as_uint(fmaf(__uint_as_float(s[c * 32 + j + u]), scale_log2e, b));
+                }
+              }
+            }
+          }
           if (need[c] && !(c * 32 >= lo && c * 32 + 32 <= hi)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
@@ -423,6 +518,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
         }
         float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         xch[((g & 1) * 2 + half) * 128 + rl] = mt;
+        if constexpr (kRel != kNoRel)  // the next tile's: both warps are past the last tile that was read from there
+          ptx::sts_2s32(pos_q + ((g + 1) & 1) * kKV * 4 + 8 * (half * 32 + lane), -4 * k0, -4 * k1);
         ptx::tc_fence_before_sync();
         ptx::named_barrier(1 + quarter, 64);  // the two warps that share these 32 rows
         if (lane == 0) ptx::mbar_arrive(bar_sfree);
@@ -431,7 +528,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
         // refer to is raised only when the true one has grown by more than kRescaleGap, so O (accumulated in
         // TMEM over all tiles) is rescaled rarely; sums and outputs are exact for any such reference value.
         mt = fmaxf(mt, xch[((g & 1) * 2 + (half ^ 1)) * 128 + rl]);
-        const float m_cand = fmaxf(m, mt * scale_log2e);  // the scale is positive: max commutes with it
+        const float m_cand = fmaxf(m, kRel != kNoRel ? mt : mt * scale_log2e);  // the scale is positive: max commutes with it
+        if (kRel != kNoRel) top = fmaxf(top, mt);
         const bool raise = m_cand > m + kRescaleGap;      // also the first tile that has a key of this row
         const float m_new = raise ? m_cand : m;
         const float m_use = m_new == -CUDART_INF_F ? 0.f : m_new;
@@ -443,8 +541,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
           if (need[c]) {
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              const float p0 = ptx::ex2_approx(fmaf(__uint_as_float(s[c * 32 + j]), scale_log2e, -m_use));  // -inf -> 0
-              const float p1 = ptx::ex2_approx(fmaf(__uint_as_float(s[c * 32 + j + 1]), scale_log2e, -m_use));
+              const float s0 = __uint_as_float(s[c * 32 + j]), s1 = __uint_as_float(s[c * 32 + j + 1]);
+              const float p0 = ptx::ex2_approx(kRel != kNoRel ? s0 - m_use : fmaf(s0, scale_log2e, -m_use));  // -inf -> 0
+              const float p1 = ptx::ex2_approx(kRel != kNoRel ? s1 - m_use : fmaf(s1, scale_log2e, -m_use));
               rs0 += p0;
               rs1 += p1;
               __nv_bfloat162 b = __floats2bfloat162_rn(p0, p1);  // low half = even key
@@ -507,7 +606,16 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       ptx::tc_fence_before_sync();
       ptx::named_barrier(1 + quarter, 64);
       const int rows = ptx::lds_s32(item_slot(it) + 68);
-      const float l_row = xl[half * 128 + rl] + xl[(half ^ 1) * 128 + rl], inv_l = 1.f / l_row;
+      const float l_row = xl[half * 128 + rl] + xl[(half ^ 1) * 128 + rl];
+      // biases of -inf may leave a row without a key: zeros
+      const float inv_l = kRel != kNoRel && l_row == 0.f ? 0.f : 1.f / l_row;
+      bool again = false;
+      if constexpr (kRel != kNoRel) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
+        again = !(sum < CUDART_INF_F) && rl < rows;
+      }
       uint4 o16[kDh / 8];
 #pragma unroll
       for (int c = 0; c < kDh / 8; ++c) {
@@ -526,7 +634,16 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
         st_global32(ao + (long long)row * C + h * D + half * kDh, o16[0], o16[1],
                     (reinterpret_cast<uintptr_t>(ao) & 31u) == 0);  // rows and heads are whole sectors then
       }
-      if (half == 0 && rl < rows) lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
+      if constexpr (kRel != kNoRel) {
+        // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, from their own keys
+        __syncwarp();
+        if (again) rel_row_again<kDh>(qkv, ao, C, h * D, half * kDh, D, row, mine.lo, mine.hi, scale_log2e, rel, h, m, inv_l);
+      }
+      if (half == 0 && rl < rows) {
+        lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
+        if (kRel != kNoRel)
+          peak[(long long)h * capacity + row] = l_row == 0.f ? 0.f : ((top - m) - log2f(l_row)) * 0.6931471805599453f;
+      }
       __syncwarp();
     }
   }
@@ -1717,6 +1834,8 @@ attn_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_c
   }
 }
 
+constexpr int kTwoPerSm = (228 * 1024 - 2 * 1024) / 2 / 16 * 16;  // shared memory of a CTA of which an SM holds two
+
 // Which kernel runs the dK / dV pass for head dimension D.
 template <int D> struct kv_pass {
   static constexpr int kThreads = kBwdThreads;
@@ -1783,14 +1902,17 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   return SPA_OK;
 }
 
-template <int D>
-int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,
-               int32_t* d_status, cudaStream_t st) {
+template <int D, int kRel>
+int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
+               float* peak, int32_t* d_status, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_tmap_bf16_2d(&tm, qkv, 3ull * p.C, p.capacity, 6ull * p.C, D, 128, D * 2)) return SPA_ERR_UNSUPPORTED;
-  auto kern = attn_fwd_tc_kernel<D>;
+  auto kern = attn_fwd_tc_kernel<D, kRel>;
+  const int smem = FwdSmem<D, kRel>::bytes(rel.pitch);
   static DeviceOnce attr;
-  cudaError_t ea = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<D>::kBytes); });
+  cudaError_t ea = attr.run([&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRel == kRelShared ? kTwoPerSm : smem);
+  });
   if (ea != cudaSuccess) { set_cuda_error(ea, "attn_fwd_tc_kernel"); return SPA_ERR_CUDA; }
   // a persistent grid: two CTAs per SM (at most 94 KB of shared memory, 256 TMEM columns each), never more than work items
   const long long items = (long long)p.H * ((p.capacity + kQ - 1) / kQ);
@@ -1798,10 +1920,19 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
   // Short segments make items of nearly the same length: putting them in order gained nothing up to segment slots of
   // 400 rows (and cost 1 us in front of short items), and 8 to 12 % from 576 rows on.
   const bool even_items = (long long)p.capacity <= 512ll * (n_seg > 0 ? n_seg : 1);
-  launch_pdl(kern, grid, kFwdThreads, FwdSmem<D>::kBytes, st, tm, seg, n_seg, p.capacity, p.C, p.H,
-             softmax_scale_of(p) * 1.4426950408889634f, (__nv_bfloat16*)ao, lse, items > grid ? item_counter(ao) : nullptr, even_items, d_status);
+  launch_pdl(kern, grid, kFwdThreads, smem, st, tm, seg, n_seg, p.capacity, p.C, p.H,
+             softmax_scale_of(p) * 1.4426950408889634f, rel, (const __nv_bfloat16*)qkv, (__nv_bfloat16*)ao, lse, peak,
+             items > grid ? item_counter(ao) : nullptr, even_items, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_fwd_tc_kernel");
   return SPA_OK;
+}
+
+template <int D>
+int rel_fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
+                   float* peak, int32_t* d_status, cudaStream_t st) {
+  if (FwdSmem<D, kRelShared>::bytes(rel.pitch) <= kTwoPerSm)
+    return fwd_launch<D, kRelShared>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
+  return fwd_launch<D, kRelGlobal>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
 }
 
 }  // namespace
@@ -1827,8 +1958,14 @@ int launch_attention_bwd_tc(const spa_params& p, const void* qkv, const void* ao
 
 int launch_attention_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,
                             int32_t* d_status, cudaStream_t st) {
-  return p.C / p.H == 64 ? fwd_launch<64>(p, qkv, seg, n_seg, ao, lse, d_status, st)
-                         : fwd_launch<32>(p, qkv, seg, n_seg, ao, lse, d_status, st);
+  return p.C / p.H == 64 ? fwd_launch<64, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, d_status, st)
+                         : fwd_launch<32, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, d_status, st);
+}
+
+int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
+                                float* lse, float* peak, int32_t* d_status, cudaStream_t st) {
+  return p.C / p.H == 64 ? rel_fwd_launch<64>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st)
+                         : rel_fwd_launch<32>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
 }
 
 }  // namespace spa
