@@ -199,7 +199,8 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
                              float* dtable, void* workspace, int32_t* d_status, cudaStream_t st) {
   const Layout l = layout(p, r);
   char* ws = static_cast<char*>(workspace);
-  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, qkv, dao, 1.f, d_status, st);
+  const bool tc = use_tc(p);
+  int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, qkv, dao, tc ? kLog2e : 1.f, d_status, st);
   if (rc != SPA_OK) return rc;
   RelGrad g = {};
   g.acc = (unsigned long long*)(ws + l.acc);
@@ -209,7 +210,8 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   g.bad = (int32_t*)(ws + l.bad);
   g.n_buckets = r.n_buckets;
   g.H = p.H;
-  rc = launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);
+  rc = tc ? launch_attention_rel_bwd_tc(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, (float*)(ws + l.delta), d_status, st)
+          : launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);
   if (rc != SPA_OK) return rc;
   const long long work = (long long)r.n_buckets * p.H > p.capacity ? (long long)r.n_buckets * p.H : p.capacity;
   const int grid = (int)((work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);

@@ -40,8 +40,8 @@ __device__ __forceinline__ int rel_exponent(float b) {
 }
 __device__ __forceinline__ float rel_scale(int e) { return __uint_as_float((uint32_t)(127 + kRelBits - e) << 23); }
 
-// 2 max |dO| max |v| of a head, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.
-__device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h) {
+// 2 max |dO| max |v| of a head, and max |v|, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.
+__device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h, float& most_v) {
   const int lane = threadIdx.x & 31;
   uint32_t v = 0, d = 0;
 #pragma unroll
@@ -54,7 +54,12 @@ __device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h) {
   }
   v = __reduce_max_sync(0xffffffffu, v);
   d = __reduce_max_sync(0xffffffffu, d);
-  return 2.f * sqrtf(__uint_as_float(v)) * sqrtf(__uint_as_float(d));
+  most_v = sqrtf(__uint_as_float(v));
+  return 2.f * most_v * sqrtf(__uint_as_float(d));
+}
+__device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h) {
+  float most_v;
+  return rel_head_bound(g, h, most_v);
 }
 
 // A row whose logarithm of the sum (NaN, +inf) or D is not finite has dS that are not
@@ -62,13 +67,17 @@ __device__ __forceinline__ void rel_check_row(const RelGrad& g, int h, float lse
   if (!(lse < __uint_as_float(0x7f800000u)) || !(fabsf(D) < __uint_as_float(0x7f800000u))) g.bad[h] = 1;
 }
 
-__device__ __forceinline__ void rel_add(const RelView& r, const RelGrad& g, int h, int off, long long v) {
-  const int b = g.bucket[off + r.center];
+// v to the bin of the bucket of table entry `at`
+__device__ __forceinline__ void rel_add(const RelGrad& g, int h, int at, long long v) {
+  const int b = g.bucket[at];
   if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)b * g.H + h, (unsigned long long)v);
 }
 
 int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
                                 float* lse, float* peak, int32_t* d_status, cudaStream_t st);
+int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
+                                const int32_t* seg, int n_seg, const RelView& view, const RelGrad& grad, void* dqkv, float* delta,
+                                int32_t* d_status, cudaStream_t st);
 int launch_attention_rel_fwd_simt(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
                                   float* lse, float* peak, cudaStream_t st);
 int launch_attention_rel_bwd_simt(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,

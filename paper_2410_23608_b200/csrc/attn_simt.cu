@@ -436,7 +436,7 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
           p = in && l != -CUDART_INF_F ? expf(fmaf(s[i][j], scale, bias[off]) - l) : 0.f;  // no key: no weight
           if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
           dp[i][j] = in ? p * (dp[i][j] - Dv) : 0.f;
-          if (dq && in) rel_add(rel, grad, h, off, __float2ll_rn(dp[i][j] * table_scale));
+          if (dq && in) rel_add(grad, h, off + rel.center, __float2ll_rn(dp[i][j] * table_scale));
         } else {
           p = in ? expf(s[i][j] * scale - l) : 0.f;
           if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;

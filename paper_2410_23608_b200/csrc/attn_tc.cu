@@ -680,23 +680,75 @@ constexpr int kBwdStatBytes = 3 * 2 * kBwdY * 4;  // three tiles' worth of lse_i
 
 // Streamed tiles in shared memory.  In the dQ pass the first of them is the memory of the O tile, which is only
 // needed for D_i before the loop starts.  A stage is as large as an own tile (two 64-row tiles).
-template <int D, bool kDQ> __host__ __device__ constexpr int bwd_stages() { return D == 32 ? 6 : (kDQ ? 4 : 3); }
-template <int D, bool kDQ> __host__ __device__ constexpr int bwd_smem_bytes() {
+// With a bias by relative position its tables take the memory of some stages.
+template <int D, bool kDQ, int kRel = kNoRel> __host__ __device__ constexpr int bwd_stages() {
+  return kRel != kNoRel ? 3 : D == 32 ? 6 : (kDQ ? 4 : 3);
+}
+constexpr int kBwdPosBytes = 3 * kBwdY * 4;  // positions of three tiles' streamed rows
+template <int D, bool kDQ, int kRel = kNoRel> __host__ __device__ constexpr int bwd_smem_bytes() {
   // two own tiles, streamed stages, alignment slack, statistics, barriers, segment offsets, row flags
-  return (2 + bwd_stages<D, kDQ>()) * 128 * D * 2 + 1024 + kBwdStatBytes + 128 + kSegStage * 4 + 64 + 128;
+  return (2 + bwd_stages<D, kDQ, kRel>()) * 128 * D * 2 + 1024 + kBwdStatBytes + 128 + kSegStage * 4 + 64 + 128 +
+         (kRel != kNoRel ? kBwdPosBytes : 0);
 }
 
-template <int D, bool kDQ, bool kLoop>
+// What the kernels with a bias by relative position are given beside the others' arguments.  shared_bins: the table's gradient is
+// summed in shared memory, item by item; else pair by pair in global memory.
+struct RelBwd {
+  RelView view;
+  RelGrad grad;
+  const __nv_bfloat16 *qkv, *dao;
+  bool shared_bins;
+};
+// The scale of an item's bins.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
+// with |dS| below 2^kRelItemBits in units of the scale a sum stays below 2^30.
+constexpr int kRelItemBits = 23;
+
+// kN head dimensions from column `col` + `first` on of a row's gradient (dQ; dK and dV) from the rows of its segment alone: rare, one
+// pair after the other from global memory.
+template <int kN>
+__device__ __noinline__ void rel_grad_again(bool dq, const RelBwd& r, const float* lse, const float* delta, __nv_bfloat16* dqkv, int C,
+                                            int capacity, int h, int d, int first, int row, int lo, int hi, float scale) {
+  const long long ld = 3LL * C;
+  const int col = h * d;
+  const float* bias = r.view.bias + (long long)h * r.view.pitch + r.view.center;
+  for (int e0 = first; e0 < first + kN; e0 += 8) {
+    float acc1[8] = {}, acc2[8] = {};
+    for (int k = lo; k < hi; ++k) {
+      const int q = dq ? row : k, j = dq ? k : row;
+      const __nv_bfloat16 *Q = r.qkv + q * ld + col, *K = r.qkv + j * ld + C + col, *dO = r.dao + (long long)q * C + col;
+      float s = 0.f, dp = 0.f;
+      for (int e = 0; e < d; ++e) {
+        s = fmaf(__bfloat162float(Q[e]), __bfloat162float(K[e]), s);
+        dp = fmaf(__bfloat162float(dO[e]), __bfloat162float(K[C + e]), dp);
+      }
+      const float l = lse[(long long)h * capacity + q];
+      const float b = bias[r.view.pos[q] - r.view.pos[j]];
+      const float p = l == -CUDART_INF_F ? 0.f : ptx::ex2_approx(fmaf(s, scale * 1.4426950408889634f, b) - l * 1.4426950408889634f);
+      const float ds = p * (dp - delta[(long long)h * capacity + q]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        acc1[e] = fmaf(ds, __bfloat162float((dq ? K : Q)[e0 + e]), acc1[e]);
+        acc2[e] = fmaf(p, __bfloat162float(dO[e0 + e]), acc2[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc1[e] *= scale;
+    *reinterpret_cast<uint4*>(dqkv + row * ld + (dq ? 0 : C) + col + e0) = Vec16<__nv_bfloat16>::from_float(acc1);
+    if (!dq) *reinterpret_cast<uint4*>(dqkv + row * ld + 2 * C + col + e0) = Vec16<__nv_bfloat16>::from_float(acc2);
+  }
+}
+
+template <int D, bool kDQ, bool kLoop, int kRel>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
                    const __grid_constant__ CUtensorMap tm_o,
                    const float* lse, float* delta, const int32_t* seg, int n_seg,
-                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, int32_t* d_status) {
+                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const RelBwd rel, int32_t* d_status) {
   using HT = HeadTile<D>;
   constexpr int kTile = HT::kTileBytes;             // own tiles: 128 rows
   constexpr int kYTile = kBwdY * HT::kRowBytes;     // streamed tiles: 64 rows
-  constexpr int kStages = bwd_stages<D, kDQ>();     // streamed stages; in the dQ pass stage 0 first holds the O tile
+  constexpr int kStages = bwd_stages<D, kDQ, kRel>();     // streamed stages; in the dQ pass stage 0 first holds the O tile
   constexpr int kShift = kDQ ? 1 : 0;               // tile t lives in stage (t + kShift) mod kStages
   static_assert(2 * kYTile == kTile, "a stage is as large as an own tile");
   constexpr float kLog2e = 1.4426950408889634f;
@@ -742,6 +794,12 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
   int32_t* seg_s = reinterpret_cast<int32_t*>(smem_al + kBarBase + 128);  // [kSegStage + 1]
   // rows of this tile whose results this kernel writes (all valid rows, or those of the long segments only)
   volatile uint8_t* row_ok = reinterpret_cast<volatile uint8_t*>(smem_al + kBarBase + 128 + kSegStage * 4 + 64);
+  // with a bias: positions of the streamed rows [3][64], the head's table (kRelShared), the item's bins (dQ pass, shared_bins)
+  constexpr int kPosBase = kBarBase + 128 + kSegStage * 4 + 64 + 128, kTableBase = kPosBase + kBwdPosBytes;
+  const uint32_t pos_s = smem_base + kPosBase, table_s = smem_base + kTableBase;
+  const uint32_t bins_s = table_s + (kRel == kRelShared ? rel.view.pitch * 4 : 0);
+  uint8_t* bins = smem_al + kTableBase + (kRel == kRelShared ? rel.view.pitch * 4 : 0);
+  uint32_t* item_bound = reinterpret_cast<uint32_t*>(smem_al + kBarBase + 104);
 
   // The thread that sets the barriers up is the one that later issues the copies counted on them.
   auto init_barriers = [&]() {
@@ -801,6 +859,17 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       ptx::tma_load_2d(x2_s, &tm_qkv, bar_x, 2 * C + h * D, r0);         // V
     }
   }
+  if constexpr (kRel != kNoRel) {  // the item before is through with all this
+    if (kRel == kRelShared) {
+      const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
+      for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<float4*>(smem_al + kTableBase)[i] = from[i];
+    }
+    if (kDQ) {
+      if (rel.shared_bins)
+        for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (tid == 0) *item_bound = 0u;
+    }
+  }
   if (first_item && warp == 0) ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t*>(tmem_slot)), kBwdTmemCols);
   first_item = false;
   ptx::tc_fence_before_sync();
@@ -856,12 +925,35 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
   // per-row statistics of the query side
   float my_lse = 0.f, my_D = 0.f;   // kDQ: this thread's query row
   float nxt_lse = 0.f, nxt_D = 0.f; // !kDQ: prefetched values of the next streamed query tile, row rl < 64
+  // -lse of a streamed query, in units of log 2; a row without a key (lse = -inf, by its biases) has no weights
+  auto stat_of = [&](int i) {
+    const float v = lse[(long long)h * capacity + i];
+    return kRel != kNoRel && v == -CUDART_INF_F ? v : -v * kLog2e;
+  };
+  int nxt_pos = 0;                  // kRel: position of row rl < 64 of the next streamed tile
+  uint32_t bias_at = 0;             // kRel: place of this thread's row in the table, bytes
+  float head_v = 0.f, row_peak = 0.f;
+  int head_exp = 0;
+  constexpr int kSign = kDQ ? -1 : 1;  // off = p_query - p_key + center
+  if constexpr (kRel != kNoRel) {
+    if (is_math) {
+      if (half == 0 && rl < kBwdY) nxt_pos = rel.view.pos[o_lo + rl];
+      bias_at = 4 * (rel.view.center - kSign * rel.view.pos[row]);
+      if (kDQ) {
+        head_exp = rel_exponent(rel_head_bound(rel.grad, h, head_v));
+        if (rel.grad.peak != nullptr && mine.hi > mine.lo) row_peak = rel.grad.peak[(long long)h * capacity + row];
+      }
+    }
+  }
   if (is_math) {
     if (kDQ) {
-      if (mine.hi > mine.lo) my_lse = lse[(long long)h * capacity + row] * kLog2e;
+      if (mine.hi > mine.lo) {
+        const float v = lse[(long long)h * capacity + row];
+        my_lse = kRel != kNoRel && v == -CUDART_INF_F ? CUDART_INF_F : v * kLog2e;
+      }
     } else if (half == 0 && rl < kBwdY) {
       const int i = o_lo + rl;
-      if (i < o_hi) { nxt_lse = -lse[(long long)h * capacity + i] * kLog2e; nxt_D = -delta[(long long)h * capacity + i]; }
+      if (i < o_hi) { nxt_lse = stat_of(i); nxt_D = -delta[(long long)h * capacity + i]; }
     }
   }
 
@@ -899,7 +991,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       stat_D[(t_ % 3) * kBwdY + rl] = nxt_D;
       const int i = y0 + kBwdY + rl;
       nxt_lse = 0.f; nxt_D = 0.f;
-      if (i < o_hi) { nxt_lse = -lse[(long long)h * capacity + i] * kLog2e; nxt_D = -delta[(long long)h * capacity + i]; }
+      if (i < o_hi) { nxt_lse = stat_of(i); nxt_D = -delta[(long long)h * capacity + i]; }
+    }
+    if (kRel != kNoRel && half == 0 && rl < kBwdY) {
+      ptx::sts_s32(pos_s + ((t_ % 3) * kBwdY + rl) * 4, kSign * 4 * nxt_pos);
+      nxt_pos = y0 + kBwdY < o_hi ? rel.view.pos[y0 + kBwdY + rl] : 0;
     }
     return ok;
   };
@@ -994,6 +1090,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     }
   } else if (!failed_early) {
     // ---------------------------------------------------------------- arithmetic: two threads per row
+    float row_norm = 0.f;  // |dO_i|^2
     if (kDQ && mine.hi > mine.lo) {
       // D_i = dO_i . O_i from the two staged tiles (their load has completed: prep(0) waited for it).  Both
       // carry the same swizzle, so equal positions hold equal columns and the order of the chunks is free:
@@ -1008,9 +1105,30 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
         Vec16<__nv_bfloat16>::to_float(*reinterpret_cast<const uint4*>(po + ((c ^ rot) << 4)), a);
         Vec16<__nv_bfloat16>::to_float(*reinterpret_cast<const uint4*>(pg + ((c ^ rot) << 4)), b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) my_D = fmaf(a[e], b[e], my_D);
+        for (int e = 0; e < 8; ++e) {
+          my_D = fmaf(a[e], b[e], my_D);
+          if (kRel != kNoRel) row_norm = fmaf(b[e], b[e], row_norm);
+        }
       }
       if (half == 0) delta[(long long)h * capacity + row] = my_D;
+    }
+    // the bins' scale: the largest bound of the item's rows (as bit patterns: a NaN is larger than every number)
+    float bin_scale = 0.f;
+    int bin_shift = 0;
+    if constexpr (kRel != kNoRel && kDQ) {
+      if (half == 0 && mine.hi > mine.lo) rel_check_row(rel.grad, h, my_lse == CUDART_INF_F ? 0.f : my_lse, my_D);
+      if (rel.shared_bins) {
+        const float b = 2.f * head_v * sqrtf(row_norm) * ptx::ex2_approx(row_peak * kLog2e);
+        const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(b) & 0x7fffffffu);
+        if (lane == 0) atomicMax(item_bound, most);
+        ptx::named_barrier(1, kBwdMath);
+        const int e = rel_exponent(__uint_as_float(*reinterpret_cast<volatile uint32_t*>(item_bound)));
+        bin_scale = __uint_as_float((uint32_t)(127 + kRelItemBits - e) << 23);
+        bin_shift = kRelBits - head_exp - (kRelItemBits - e);
+        if (tid == 0) range[0] = bin_shift;  // everyone has read its own copy: o_lo
+      } else {
+        bin_scale = rel_scale(head_exp);
+      }
     }
 
     constexpr int kPc = kBwdY / 2;  // fp32 columns of each tile owned by this thread
@@ -1033,7 +1151,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       if (ok && t + 1 < n_tiles) ok = prep(t + 1);
       // the statistics of tile t were staged by other warps before they announced tile t - 1 (that phase has
       // completed; it is waited for, before this warp's own arrival for tile t, to order the reads below)
-      if (ok && !kDQ && t > 0) ok = wait_w(bar_sfree, (t - 1) & 1);
+      if (ok && (!kDQ || kRel != kNoRel) && t > 0) ok = wait_w(bar_sfree, (t - 1) & 1);
       if (!ok) { fail(); break; }
       ptx::tc_fence_before_sync();
       __syncwarp();
@@ -1044,6 +1162,21 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       const int yc0 = y0 + col0;
       uint32_t pk_p[kPc / 2], pk_ds[kPc / 2];
       if (yc0 < mine.hi && yc0 + kPc > mine.lo) {
+        const uint32_t pos_at = pos_s + ((t % 3) * kBwdY + col0) * 4;
+        if constexpr (kRel != kNoRel) {  // S in units of log 2, with its bias
+          const char* table = reinterpret_cast<const char*>(rel.view.bias + (long long)h * rel.view.pitch);
+#pragma unroll
+          for (int j = 0; j < kPc; j += 4) {
+            int k[4];
+            ptx::lds_4s32(pos_at + 4 * j, k);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float b = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u])
+                                                 : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
+              rs[j + u] = __float_as_uint(fmaf(__uint_as_float(rs[j + u]), scale_log2e, b));
+            }
+          }
+        }
         if (!(yc0 >= mine.lo && yc0 + kPc <= mine.hi)) {
 #pragma unroll
           for (int j = 0; j < kPc; ++j)
@@ -1057,7 +1190,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
           const uint64_t scale2 = ptx::pair(scale_log2e, scale_log2e), lse2 = ptx::pair(-my_lse, -my_lse), D2 = ptx::pair(-my_D, -my_D);
 #pragma unroll
           for (int j = 0; j < kPc; j += 2) {
-            ptx::unpair(ptx::fma2(ptx::pair(rs[j], rs[j + 1]), scale2, lse2), rs[j], rs[j + 1]);
+            if (kRel != kNoRel) ptx::unpair(ptx::add2(ptx::pair(rs[j], rs[j + 1]), lse2), rs[j], rs[j + 1]);
+            else ptx::unpair(ptx::fma2(ptx::pair(rs[j], rs[j + 1]), scale2, lse2), rs[j], rs[j + 1]);
             ptx::unpair(ptx::add2(ptx::pair(rp[j], rp[j + 1]), D2), rp[j], rp[j + 1]);
           }
 #pragma unroll
@@ -1067,6 +1201,23 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
             float d0, d1;
             ptx::unpair(ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1])), d0, d1);
             pk_ds[j >> 1] = ptx::bf16_pair(d0, d1);
+            if (kRel != kNoRel) { rs[j] = __float_as_uint(d0); rs[j + 1] = __float_as_uint(d1); }
+          }
+          if constexpr (kRel != kNoRel) {  // the table's gradient: a pair's bin is where its bias came from
+#pragma unroll
+            for (int j = 0; j < kPc; j += 4) {
+              int k[4];
+              ptx::lds_4s32(pos_at + 4 * j, k);
+              if (rel.shared_bins) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rs[j + u]) * bin_scale));
+              } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  rel_add(rel.grad, h, (int)(bias_at + k[u]) >> 2, __float2ll_rn(__uint_as_float(rs[j + u]) * bin_scale));
+              }
+            }
           }
         } else {
           const float* sl = stat_lse + (t % 3) * kBwdY + col0;
@@ -1076,7 +1227,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
             float pv[2], dsv[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              pv[u] = ptx::ex2_approx(fmaf(__uint_as_float(rs[j + u]), scale_log2e, sl[j + u]));
+              pv[u] = ptx::ex2_approx(kRel != kNoRel ? __uint_as_float(rs[j + u]) + sl[j + u]
+                                                     : fmaf(__uint_as_float(rs[j + u]), scale_log2e, sl[j + u]));
               dsv[u] = pv[u] * (__uint_as_float(rp[j + u]) + sd[j + u]);
             }
             pk_ds[j >> 1] = ptx::bf16_pair(dsv[0], dsv[1]);
@@ -1114,12 +1266,19 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
+    bool again = false;
     auto stage_acc = [&](uint32_t acc_col, uint8_t* tile, float mul) {
       uint32_t r[kDh];
       if (kDh == 32) ptx::tmem_ld_32x32(tmem + lane_base + acc_col + half * kDh, r);
       else ptx::tmem_ld_32x16(tmem + lane_base + acc_col + half * kDh, r);
       ptx::tmem_ld_wait();
       const int rot = chunk_rot<D>(rl);
+      if (kRel != kNoRel) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
+        again = again || !(sum < CUDART_INF_F);
+      }
 #pragma unroll
       for (int g = 0; g < kDh / 8; ++g) {
         float v[8];
@@ -1142,6 +1301,20 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       __syncthreads();
       copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
       copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
+    }
+    if constexpr (kRel != kNoRel) {
+      if (kDQ && rel.shared_bins) {  // the item's bins to the head's sums
+        const int shift = range[0];
+        for (int i = tid; i < rel.view.entries; i += kBwdThreads) {
+          const int v = reinterpret_cast<int*>(bins)[i];
+          if (v != 0) rel_add(rel.grad, h, i, shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63));
+        }
+      }
+      // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, from their own segment
+      if (__syncthreads_or(again)) {
+        if (again && mine.hi > mine.lo)
+          rel_grad_again<kDh>(kDQ, rel, lse, delta, dqkv, C, capacity, h, D, half * kDh, row, mine.lo, mine.hi, scale);
+      }
     }
   }
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
@@ -1167,18 +1340,19 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
 // queues S^T(t+1) (once every arithmetic warp holds S^T(t) in registers), dV(t) (P^T(t) written), dK(t) (dS^T(t)
 // stored) and dP^T(t+1), the last behind dK(t), which reads the columns it overwrites.
 constexpr int kSplitStages = 3;  // streamed stages of a 64-row Q tile and a 64-row dO tile
-template <int D> __host__ __device__ constexpr int split_smem_bytes() {
+template <int D, int kRel = kNoRel> __host__ __device__ constexpr int split_smem_bytes() {
   // own K and V, streamed stages, P^T, alignment slack, statistics, barriers, segment offsets, row flags
-  return (2 + kSplitStages) * 128 * D * 2 + 128 * kBwdY * 2 + 1024 + kBwdStatBytes + 128 + kSegStage * 4 + 64 + 128;
+  return (2 + kSplitStages) * 128 * D * 2 + 128 * kBwdY * 2 + 1024 + kBwdStatBytes + 128 + kSegStage * 4 + 64 + 128 +
+         (kRel != kNoRel ? kBwdPosBytes : 0);
 }
 
-template <int D, bool kLoop>
+template <int D, bool kLoop, int kRel>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
                    const __grid_constant__ CUtensorMap tm_o,
                    const float* lse, float* delta, const int32_t* seg, int n_seg,
-                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, int32_t* d_status) {
+                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const RelBwd rel, int32_t* d_status) {
   using HT = HeadTile<D>;
   constexpr int kTile = HT::kTileBytes;             // own tiles: 128 rows
   constexpr int kYTile = kBwdY * HT::kRowBytes;     // streamed tiles: 64 rows
@@ -1223,6 +1397,9 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
   int32_t* seg_s = reinterpret_cast<int32_t*>(smem_al + kBarBase + 128);  // [kSegStage + 1]
   // rows of this tile whose results this kernel writes (all valid rows, or those of the long segments only)
   volatile uint8_t* row_ok = reinterpret_cast<volatile uint8_t*>(smem_al + kBarBase + 128 + kSegStage * 4 + 64);
+  // with a bias: positions of the streamed rows [3][64], the head's table (kRelShared)
+  constexpr int kPosBase = kBarBase + 128 + kSegStage * 4 + 64 + 128, kTableBase = kPosBase + kBwdPosBytes;
+  const uint32_t pos_s = smem_base + kPosBase, table_s = smem_base + kTableBase;
 
   // The thread that sets the barriers up is the one that later issues the copies counted on them.
   auto init_barriers = [&]() {
@@ -1279,6 +1456,10 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     ptx::tma_load_2d(x1_s, &tm_qkv, bar_x, x1_col, r0);
     ptx::tma_load_2d(x2_s, &tm_qkv, bar_x, 2 * C + h * D, r0);           // V
   }
+  if constexpr (kRel == kRelShared) {  // the item before is through with it
+    const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
+    for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<float4*>(smem_al + kTableBase)[i] = from[i];
+  }
   if (first_item && warp == 0) ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t*>(tmem_slot)), kBwdTmemCols);
   first_item = false;
   ptx::tc_fence_before_sync();
@@ -1332,9 +1513,20 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
 
   // per-row statistics of the query side
   float nxt_lse = 0.f, nxt_D = 0.f;  // prefetched values of the next streamed query tile, row rl < 64
+  // -lse of a streamed query, in units of log 2; a row without a key (lse = -inf, by its biases) has no weights
+  auto stat_of = [&](int i) {
+    const float v = lse[(long long)h * capacity + i];
+    return kRel != kNoRel && v == -CUDART_INF_F ? v : -v * kLog2e;
+  };
+  int nxt_pos = 0;       // kRel: position of row rl < 64 of the next streamed tile
+  uint32_t bias_at = 0;  // kRel: place of this thread's row in the table, bytes: off = p_query - p_key + center
+  if (kRel != kNoRel && is_math) {
+    if (half == 0 && rl < kBwdY) nxt_pos = rel.view.pos[o_lo + rl];
+    bias_at = 4 * (rel.view.center - rel.view.pos[row]);
+  }
   if (is_math && half == 0 && rl < kBwdY) {
     const int i = o_lo + rl;
-    if (i < o_hi) { nxt_lse = -lse[(long long)h * capacity + i] * kLog2e; nxt_D = -delta[(long long)h * capacity + i]; }
+    if (i < o_hi) { nxt_lse = stat_of(i); nxt_D = -delta[(long long)h * capacity + i]; }
   }
 
   constexpr uint32_t kIdescS = ptx::idesc_bf16_f32(128, kBwdY, false, false);
@@ -1369,7 +1561,11 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
       stat_D[(t_ % 3) * kBwdY + rl] = nxt_D;
       const int i = y0 + kBwdY + rl;
       nxt_lse = 0.f; nxt_D = 0.f;
-      if (i < o_hi) { nxt_lse = -lse[(long long)h * capacity + i] * kLog2e; nxt_D = -delta[(long long)h * capacity + i]; }
+      if (i < o_hi) { nxt_lse = stat_of(i); nxt_D = -delta[(long long)h * capacity + i]; }
+    }
+    if (kRel != kNoRel && half == 0 && rl < kBwdY) {
+      ptx::sts_s32(pos_s + ((t_ % 3) * kBwdY + rl) * 4, 4 * nxt_pos);
+      nxt_pos = y0 + kBwdY < o_hi ? rel.view.pos[y0 + kBwdY + rl] : 0;
     }
     return ok;
   };
@@ -1490,6 +1686,21 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
       const bool partial = some && !(yc0 >= mine.lo && yc0 + kPc <= mine.hi);
       uint32_t pk[kPc / 2];
       if (some) {
+        if constexpr (kRel != kNoRel) {  // S in units of log 2, with its bias
+          const char* table = reinterpret_cast<const char*>(rel.view.bias + (long long)h * rel.view.pitch);
+          const uint32_t pos_at = pos_s + ((t % 3) * kBwdY + col0) * 4;
+#pragma unroll
+          for (int j = 0; j < kPc; j += 4) {
+            int k[4];
+            ptx::lds_4s32(pos_at + 4 * j, k);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float b = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u])
+                                                 : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
+              rs[j + u] = __float_as_uint(fmaf(__uint_as_float(rs[j + u]), scale_log2e, b));
+            }
+          }
+        }
         if (partial) {
 #pragma unroll
           for (int j = 0; j < kPc; ++j)
@@ -1502,8 +1713,13 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
         for (int j = 0; j < kPc; j += 4) {
           uint64_t l2[2];
           ptx::lds_pairs(sl + j * 4, l2[0], l2[1]);
-          ptx::unpair(ptx::fma2(ptx::pair(rs[j], rs[j + 1]), scale2, l2[0]), rs[j], rs[j + 1]);
-          ptx::unpair(ptx::fma2(ptx::pair(rs[j + 2], rs[j + 3]), scale2, l2[1]), rs[j + 2], rs[j + 3]);
+          if (kRel != kNoRel) {
+            ptx::unpair(ptx::add2(ptx::pair(rs[j], rs[j + 1]), l2[0]), rs[j], rs[j + 1]);
+            ptx::unpair(ptx::add2(ptx::pair(rs[j + 2], rs[j + 3]), l2[1]), rs[j + 2], rs[j + 3]);
+          } else {
+            ptx::unpair(ptx::fma2(ptx::pair(rs[j], rs[j + 1]), scale2, l2[0]), rs[j], rs[j + 1]);
+            ptx::unpair(ptx::fma2(ptx::pair(rs[j + 2], rs[j + 3]), scale2, l2[1]), rs[j + 2], rs[j + 3]);
+          }
         }
 #pragma unroll
         for (int j = 0; j < kPc; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
@@ -1565,12 +1781,19 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
+    bool again = false;
     auto stage_acc = [&](uint32_t acc_col, uint8_t* tile, float mul) {
       uint32_t r[kDh];
       if (kDh == 32) ptx::tmem_ld_32x32(tmem + lane_base + acc_col + half * kDh, r);
       else ptx::tmem_ld_32x16(tmem + lane_base + acc_col + half * kDh, r);
       ptx::tmem_ld_wait();
       const int rot = chunk_rot<D>(rl);
+      if (kRel != kNoRel) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
+        again = again || !(sum < CUDART_INF_F);
+      }
 #pragma unroll
       for (int g = 0; g < kDh / 8; ++g) {
         float v[8];
@@ -1588,6 +1811,12 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     __syncthreads();
     copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
     copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
+    if constexpr (kRel != kNoRel) {  // see the dQ pass
+      if (__syncthreads_or(again)) {
+        if (again && mine.hi > mine.lo)
+          rel_grad_again<kDh>(false, rel, lse, delta, dqkv, C, capacity, h, D, half * kDh, row, mine.lo, mine.hi, scale);
+      }
+    }
   }
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
     for (int t = issued > kStages ? issued - kStages : 0; t < issued; ++t) ptx::mbar_wait(bar_y(stage_of(t)), use_of(t));
@@ -1835,22 +2064,25 @@ attn_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_c
 }
 
 constexpr int kTwoPerSm = (228 * 1024 - 2 * 1024) / 2 / 16 * 16;  // shared memory of a CTA of which an SM holds two
+constexpr int kOnePerSm = 227 * 1024;
 
 // Which kernel runs the dK / dV pass for head dimension D.
-template <int D> struct kv_pass {
+template <int D, int kRel> struct kv_pass {
   static constexpr int kThreads = kBwdThreads;
-  static constexpr int kSmem = bwd_smem_bytes<D, false>();
-  template <bool kLoop> static auto kernel() { return attn_bwd_tc_kernel<D, false, kLoop>; }
+  static constexpr int kSmem = bwd_smem_bytes<D, false, kRel>();
+  template <bool kLoop> static auto kernel() { return attn_bwd_tc_kernel<D, false, kLoop, kRel>; }
 };
-template <> struct kv_pass<64> {
+template <int kRel> struct kv_pass<64, kRel> {
   static constexpr int kThreads = kBwdThreads;
-  static constexpr int kSmem = split_smem_bytes<64>();
-  template <bool kLoop> static auto kernel() { return attn_bwd_kv_split_kernel<64, kLoop>; }
+  static constexpr int kSmem = split_smem_bytes<64, kRel>();
+  template <bool kLoop> static auto kernel() { return attn_bwd_kv_split_kernel<64, kLoop, kRel>; }
 };
 
-template <int D>
+// kRel: rel is used, and the memory that the tables need is added to the kernels' own.  The bins of the dQ pass come first (kRelGlobal:
+// they may take a whole SM's memory), then the table.
+template <int D, int kRel>
 int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
-               const int32_t* seg, int n_seg, void* dqkv, void* workspace, int32_t* d_status, cudaStream_t st) {
+               const int32_t* seg, int n_seg, void* dqkv, void* workspace, RelBwd rel, int32_t* d_status, cudaStream_t st) {
   CUtensorMap tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o;  // own tiles: 128-row boxes; streamed tiles: 64-row boxes
   if (!make_tmap_bf16_2d(&tm_qkv, qkv, 3ull * p.C, p.capacity, 6ull * p.C, D, 128, D * 2) ||
       !make_tmap_bf16_2d(&tm_do, dao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, 128, D * 2) ||
@@ -1858,14 +2090,25 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
       !make_tmap_bf16_2d(&tm_do_y, dao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, kBwdY, D * 2) ||
       !make_tmap_bf16_2d(&tm_o, ao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, 128, D * 2))
     return SPA_ERR_UNSUPPORTED;
+  using KV = kv_pass<D, kRel>;
+  const int table = kRel == kNoRel ? 0 : rel.view.pitch * 4;
+  int dq_smem = bwd_smem_bytes<D, true, kRel>() + (kRel == kRelShared ? 2 * table : 0);
+  if (kRel == kRelShared) rel.shared_bins = true;
+  if (kRel == kRelGlobal) {
+    rel.shared_bins = dq_smem + table <= kOnePerSm;
+    if (rel.shared_bins) dq_smem += table;
+  }
+  const int kv_smem = KV::kSmem + (kRel == kRelShared ? table : 0);
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] {
     const auto smem_attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    cudaError_t e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, false>, smem_attr, bwd_smem_bytes<D, true>());
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, true>, smem_attr, bwd_smem_bytes<D, true>());
+    constexpr int kDqMost = kRel == kRelGlobal ? kOnePerSm : kRel == kRelShared ? kTwoPerSm : bwd_smem_bytes<D, true>();
+    constexpr int kKvMost = kRel == kRelShared ? kTwoPerSm : KV::kSmem;
+    cudaError_t e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, false, kRel>, smem_attr, kDqMost);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, true, kRel>, smem_attr, kDqMost);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_bwd_short_kernel<D>, smem_attr, short_smem_bytes<D>());
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_pass<D>::template kernel<false>(), smem_attr, kv_pass<D>::kSmem);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(kv_pass<D>::template kernel<true>(), smem_attr, kv_pass<D>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(KV::template kernel<false>(), smem_attr, kKvMost);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(KV::template kernel<true>(), smem_attr, kKvMost);
   });
   if (ea != cudaSuccess) { set_cuda_error(ea, "attn_bwd_tc_kernel"); return SPA_ERR_CUDA; }
   float* delta = reinterpret_cast<float*>(workspace);  // [H][capacity]
@@ -1879,25 +2122,25 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   const bool even_items = (long long)p.capacity <= 256ll * (n_seg > 0 ? n_seg : 1);
   const bool loop = even_items && items >= 3ll * 2 * kNumSMs;
   const int grid = (int)(loop ? 2 * kNumSMs : items);
-  auto kq = loop ? attn_bwd_tc_kernel<D, true, true> : attn_bwd_tc_kernel<D, true, false>;
-  auto kkv = loop ? kv_pass<D>::template kernel<true>() : kv_pass<D>::template kernel<false>();
+  auto kq = loop ? attn_bwd_tc_kernel<D, true, true, kRel> : attn_bwd_tc_kernel<D, true, false, kRel>;
+  auto kkv = loop ? KV::template kernel<true>() : KV::template kernel<false>();
   const float scale = softmax_scale_of(p);
   // Under SPA_FLAG_ONE_PASS_BWD segments of at most 128 rows go to the one-pass kernel (one CTA per segment and
   // head) and the two passes take the longer ones; otherwise, or with more segments than a grid dimension holds, the
   // two passes take everything.
-  const int skip_short = ((p.flags & SPA_FLAG_ONE_PASS_BWD) && n_seg >= 1 && n_seg <= 65535) ? 1 : 0;
+  const int skip_short = (kRel == kNoRel && (p.flags & SPA_FLAG_ONE_PASS_BWD) && n_seg >= 1 && n_seg <= 65535) ? 1 : 0;
   if (skip_short) {
     launch_pdl(attn_bwd_short_kernel<D>, dim3(p.H, n_seg), kShortThreads, short_smem_bytes<D>(), st, tm_qkv, tm_do, tm_o, lse,
                seg, n_seg, p.capacity, p.C, scale, (__nv_bfloat16*)dqkv, d_status);
     SPA_CUDA_CHECK_LAUNCH("attn_bwd_short_kernel");
   }
-  launch_pdl(kq, grid, kBwdThreads, bwd_smem_bytes<D, true>(), st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
-             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, d_status);
+  launch_pdl(kq, grid, kBwdThreads, dq_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
+             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dQ)");
-  if (attention_bwd_kv_applies(p, n_seg))
+  if (kRel == kNoRel && attention_bwd_kv_applies(p, n_seg))
     return launch_attention_bwd_kv(p, qkv, lse, delta, dao, seg, n_seg, dqkv, skip_short != 0, d_status, st);
-  launch_pdl(kkv, grid, kv_pass<D>::kThreads, kv_pass<D>::kSmem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
-             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, d_status);
+  launch_pdl(kkv, grid, KV::kThreads, kv_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
+             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dKV)");
   return SPA_OK;
 }
@@ -1952,8 +2195,23 @@ size_t tc_attention_workspace_bytes(const spa_params& p) {
 int launch_attention_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                             const int32_t* seg, int n_seg, void* dqkv, void* workspace, int32_t* d_status,
                             cudaStream_t st) {
-  return p.C / p.H == 64 ? bwd_launch<64>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, d_status, st)
-                         : bwd_launch<32>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, d_status, st);
+  return p.C / p.H == 64 ? bwd_launch<64, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, d_status, st)
+                         : bwd_launch<32, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, d_status, st);
+}
+
+int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
+                                const int32_t* seg, int n_seg, const RelView& view, const RelGrad& grad, void* dqkv, float* delta,
+                                int32_t* d_status, cudaStream_t st) {
+  const RelBwd rel{view, grad, (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, true};
+  const int table = view.pitch * 4;
+  if (p.C / p.H == 64) {
+    if (bwd_smem_bytes<64, true, kRelShared>() + 2 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
+      return bwd_launch<64, kRelShared>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
+    return bwd_launch<64, kRelGlobal>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
+  }
+  if (bwd_smem_bytes<32, true, kRelShared>() + 2 * table <= kTwoPerSm && bwd_smem_bytes<32, false, kRelShared>() + table <= kTwoPerSm)
+    return bwd_launch<32, kRelShared>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
+  return bwd_launch<32, kRelGlobal>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
 }
 
 int launch_attention_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,

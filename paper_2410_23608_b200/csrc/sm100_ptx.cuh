@@ -110,6 +110,9 @@ __device__ __forceinline__ void sts_2s32(uint32_t addr, int a, int b) {
 __device__ __forceinline__ void lds_4s32(uint32_t addr, int (&v)[4]) {  // a 16-byte boundary
   asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void red_add_s32(uint32_t addr, int v) {
+  asm volatile("red.shared.add.s32 [%0], %1;" ::"r"(addr), "r"(v));
+}
 // Plain values that other threads have written before a barrier: may be moved, but not across what clobbers memory
 __device__ __forceinline__ float lds_f32(uint32_t addr) {
   float v;
