@@ -9,19 +9,32 @@
 // B_b = sum d over its rows: dgate_b = scale (g_post A_b + b_post B_b), A = sum_b gate_b A_b.  So four running sums per channel
 // (the other two: sum dn yh, sum dn) in registers serve six gradients.
 //
-// Both directions are bound by bytes: every operand is read once, every result written once, all loads of a row are issued
-// together.  A row belongs to a group of W warps, sized so that a thread holds one to four 16-byte chunks (two in the
-// backward, whose running sums take 32 registers a chunk).  Statistics and sums are fp32; y and n are rounded once, n from the
-// unrounded y.  Sums run in a fixed order: results are bitwise reproducible.
+// Both directions are bound by bytes, and nearly as much by the instructions on a row: in the backward's first form, every value
+// converted and every parameter read again in each of its three steps, 18 432 rows of 768 took 102 us against 26 for their
+// bytes.  So a row belongs to as many warps as leave a thread one 16-byte chunk (two beyond 512 chunks), arithmetic is on pairs of
+// fp32, products of parameters are held in registers, and the next row's loads are on their way under the arithmetic of
+// a row.  Statistics and sums are fp32; y and n are rounded once, n from the unrounded y.  Sums run in a fixed order: results
+// are bitwise reproducible.
+#include "simt_stage.cuh"
+#include "sm100_ptx.cuh"
 #include "spa_common.cuh"
 
 namespace spa {
 namespace {
 
+using ptx::add2;
+using ptx::fma2;
+using ptx::mul2;
+using ptx::pair;
+using ptx::unpair;
+
 constexpr int kMaxChunks = 1024;  // 16-byte chunks of a row: 8 192 bf16 or 4 096 fp32 channels
 constexpr int kSums = 4;          // running sums per channel of the backward: A, B, sum dn yh, sum dn
-template <int W> constexpr int kThreads = W == 16 ? 512 : 256;
-template <int W> constexpr int kGroups = kThreads<W> / (32 * W);
+// Rows that a CTA has under way with W warps to a row, and its threads.  Backward: one CTA per SM, whose sums are one line to join.
+__host__ __device__ constexpr int groups_of(int W, bool bwd) {
+  return bwd ? (W == 1 ? 16 : W == 2 ? 8 : W == 3 ? 5 : W == 4 ? 4 : W <= 8 ? 16 / W : 1) : (W == 1 ? 8 : W == 2 ? 4 : W == 3 ? 3 : W <= 6 ? 2 : 1);
+}
+__host__ __device__ constexpr int threads_of(int W, bool bwd) { return 32 * W * groups_of(W, bwd); }
 
 struct Args {
   const uint4 *x, *z, *dn, *dy, *y;   // rows of Q chunks; dn, dy optional
@@ -30,143 +43,276 @@ struct Args {
   const uint4 *scale, *g_post, *b_post, *g_pre, *b_pre;  // optional
   float* stats;                       // [4][rows]: mean and 1 / deviation of z's row, of y's
   uint4 *out_y, *out_n;               // forward
-  uint4 *dx, *dz;                     // backward; dz optional
+  uint4 *dx, *dz;                     // backward
   void* dgate;
   float *part, *part_gate;            // per CTA [kSums][C]; per unit of an image's rows [2][C]
-  int rows, N, Q, C, z_rows, kind, gate_kind, units, splits;
+  int rows, N, Q, C, z_rows, kind, rows_per_cta;
+  bool gate_f32;                      // dgate of a gate per token: fp32
   float eps;
 };
 
-// Sums of a and b over the group's threads, in every one of them.  Calls alternate between two lines of `red`: a warp that
+// The rows that a group has on their way, in shared memory: a thread copies its own chunks of the kA arrays of a row, asynchronously,
+// kDepth rows ahead (registers hold one row ahead at most: 16 rows of 1.5 KB per SM in flight instead of 64, 18 432 rows of 768
+// backward 47 us), and its warp's first lanes the row's scalars.  Nobody else reads them but the warp.
+template <int kA, int kCh, int kDepth, int kThreads> struct Ring {
+  static constexpr int kSlot = kA * kCh * kThreads * 16, kScalars = kThreads / 32 * 32;
+  static constexpr int kBytes = kDepth * (kSlot + kScalars);
+  uint8_t* base;
+  int slot;
+  __device__ __forceinline__ uint8_t* chunk(int array, int k) const {
+    return base + slot * kSlot + ((array * kCh + k) * kThreads + (int)threadIdx.x) * 16;
+  }
+  __device__ __forceinline__ float* scalars() const {  // eight of this warp
+    return reinterpret_cast<float*>(base + kDepth * kSlot + slot * kScalars) + (threadIdx.x >> 5) * 8;
+  }
+  __device__ __forceinline__ void copy(int array, int k, const uint4* from) const {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(chunk(array, k))), "l"(__cvta_generic_to_global(from)) : "memory");
+  }
+  __device__ __forceinline__ void copy_scalar(int i, const float* from) const {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(scalars() + i)), "l"(__cvta_generic_to_global(from)) : "memory");
+  }
+  __device__ __forceinline__ uint4 get(int array, int k) const { return *reinterpret_cast<const uint4*>(chunk(array, k)); }
+  __device__ __forceinline__ void next() { slot = slot + 1 == kDepth ? 0 : slot + 1; }
+};
+
+// Sums of kN values over the group's threads, in every one of them.  Calls alternate between two lines of `red`: a warp that
 // writes a line again has met the others at the barrier in between, behind their reads of it.
 template <int W> struct GroupSum {
-  float* red;  // [2][W][2] of this group
+  float* red;  // [2][W][4] of this group
   int id, warp, lane, turn;
-  __device__ __forceinline__ void operator()(float& a, float& b) {
+  template <int kN> __device__ __forceinline__ void operator()(float (&v)[kN]) {
+    static_assert(kN <= 3, "a line has room for four");
+    // two values at once: half of the lanes carries each of them through the last four steps
+    if constexpr (kN >= 2) {
+      const bool up = (lane & 16) != 0;
+      float s = up ? v[1] : v[0];
+      s += __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, o);
-      b += __shfl_xor_sync(0xffffffffu, b, o);
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      v[0] = v[1] = s;
+      if constexpr (W == 1) {
+        const float t = __shfl_xor_sync(0xffffffffu, s, 16);
+        v[0] = up ? t : s;
+        v[1] = up ? s : t;
+      }
+    }
+    if constexpr (kN != 2) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v[kN - 1] += __shfl_xor_sync(0xffffffffu, v[kN - 1], o);
     }
     if constexpr (W > 1) {
-      float* line = red + turn * 2 * W;
-      if (lane == 0) { line[2 * warp] = a; line[2 * warp + 1] = b; }
+      float* line = red + turn * 4 * W;
+      if (lane == 0) line[4 * warp] = v[0];
+      if (kN >= 2 && lane == 16) line[4 * warp + 1] = v[1];
+      if (kN == 3 && lane == 0) line[4 * warp + 2] = v[2];
       asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "n"(32 * W) : "memory");
-      a = b = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) { a += line[2 * w]; b += line[2 * w + 1]; }
+      for (int i = 0; i < kN; ++i) v[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float4 l = *reinterpret_cast<const float4*>(line + 4 * w);
+        v[0] += l.x;
+        if (kN >= 2) v[1] += l.y;
+        if (kN == 3) v[2] += l.z;
+      }
       turn ^= 1;
     }
   }
 };
 
-template <typename T> __device__ __forceinline__ void chunk_or(const uint4* p, int q, float fill, float* f) {
-  if (p != nullptr) {
-    Vec16<T>::to_float(p[q], f);
+// A chunk as pairs of fp32 and back
+template <typename T> constexpr int kPairs = Vec16<T>::kElems / 2;
+__device__ __forceinline__ void to_pairs(const uint4& v, uint64_t (&p)[2]) {
+  p[0] = pair(v.x, v.y);
+  p[1] = pair(v.z, v.w);
+}
+__device__ __forceinline__ void to_pairs(const uint4& v, uint64_t (&p)[4]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = pair(w[i] << 16, w[i] & 0xffff0000u);
+}
+__device__ __forceinline__ uint4 from_pairs(const uint64_t (&p)[2]) {
+  uint4 v;
+  unpair(p[0], v.x, v.y);
+  unpair(p[1], v.z, v.w);
+  return v;
+}
+__device__ __forceinline__ uint4 from_pairs(const uint64_t (&p)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpair(p[i], a, b);
+    w[i] = ptx::bf16_pair(a, b);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ float sum_of(uint64_t p) {
+  float a, b;
+  unpair(p, a, b);
+  return a + b;
+}
+
+// A chunk of a parameter, `fill` where it is absent
+template <typename T> __device__ __forceinline__ void param(const uint4* p, int q, bool in, float fill, uint64_t (&v)[kPairs<T>]) {
+  if (p != nullptr && in) {
+    to_pairs(p[q], v);
   } else {
 #pragma unroll
-    for (int e = 0; e < Vec16<T>::kElems; ++e) f[e] = fill;
+    for (int i = 0; i < kPairs<T>; ++i) v[i] = both(fill);
   }
 }
 
 __device__ __forceinline__ float sigmoid(float s) { return 1.f / (1.f + expf(-s)); }
 
-template <typename T, int W, int kCh>
-__global__ void __launch_bounds__(kThreads<W>) sandwich_fwd_kernel(const Args a) {
+template <int kGate> constexpr bool kGateRows = kGate == SPA_GATE_IMAGE || kGate == SPA_GATE_TOKEN;  // gates of C values
+
+template <int kGate> constexpr int kFwdArrays = kGateRows<kGate> ? 3 : 2;
+constexpr int kFwdDepth = 4;
+
+template <typename T, int W, int kCh, int kGate>
+__global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(const Args a) {
   pdl_entry();
-  constexpr int E = Vec16<T>::kElems, G = 32 * W;
-  __shared__ float red[kGroups<W> * 4 * W];
+  constexpr int P = kPairs<T>, G = 32 * W;
+  __shared__ __align__(16) float red[groups_of(W, false) * 8 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  GroupSum<W> sum{red + grp * 4 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
+  GroupSum<W> sum{red + grp * 8 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
   const float inv_c = 1.f / a.C;
   const bool layer = a.kind == SPA_NORM_LAYER;
-  // mean (0 for RMS) and 1 / deviation of the row v
-  auto statistics = [&](const float (&v)[kCh][E], float& mean, float& rstd) {
-    float s = 0.f, none = 0.f;
+  // y = x + gate (cw zh + cb), n = cp norm(y) + bp
+  uint64_t cw[kCh][P], cb[kCh][P], cp[kCh][P], bp[kCh][P];
+#pragma unroll
+  for (int k = 0; k < kCh; ++k) {
+    const int q = t0 + G * k;
+    const bool in = q < a.Q;
+    uint64_t sc[P];
+    param<T>(a.scale, q, in, 1.f, sc);
+    param<T>(a.g_post, q, in, 1.f, cw[k]);
+    param<T>(a.b_post, q, in, 0.f, cb[k]);
+    param<T>(a.g_pre, q, in, 1.f, cp[k]);
+    param<T>(a.b_pre, q, in, 0.f, bp[k]);
+#pragma unroll
+    for (int i = 0; i < P; ++i) { cw[k][i] = mul2(cw[k][i], sc[i]); cb[k][i] = mul2(cb[k][i], sc[i]); }
+  }
+  // mean (0 for RMS) and 1 / deviation of the row v, whose chunks past the end are zero
+  auto statistics = [&](const uint64_t (&v)[kCh][P], float& mean, float& rstd) {
     mean = 0.f;
     if (layer) {
+      uint64_t s = 0ull;
 #pragma unroll
       for (int k = 0; k < kCh; ++k)
-        if (t0 + G * k < a.Q) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) s += v[k][e];
-        }
-      sum(s, none);
-      mean = s * inv_c;
+        for (int i = 0; i < P; ++i) s = add2(s, v[k][i]);
+      float t[1] = {sum_of(s)};
+      sum(t);
+      mean = t[0] * inv_c;
     }
-    float ss = 0.f;
-    none = 0.f;
+    const uint64_t m = both(-mean);
+    uint64_t ss = 0ull;
 #pragma unroll
     for (int k = 0; k < kCh; ++k)
       if (t0 + G * k < a.Q) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) { const float d = v[k][e] - mean; ss = fmaf(d, d, ss); }
+        for (int i = 0; i < P; ++i) { const uint64_t d = add2(v[k][i], m); ss = fma2(d, d, ss); }
       }
-    sum(ss, none);
-    rstd = rsqrtf(ss * inv_c + a.eps);
+    float t[1] = {sum_of(ss)};
+    sum(t);
+    rstd = rsqrtf(t[0] * inv_c + a.eps);
   };
-  for (int t = blockIdx.x * kGroups<W> + grp; t < a.rows; t += gridDim.x * kGroups<W>) {
-    int zr = t;
-    if (a.z_row != nullptr) zr = ld_dep(a.z_row + t);
-    const bool has = zr >= 0 && zr < a.z_rows;
-    const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
-    uint4 xr[kCh], zv[kCh], gr[kCh];
-    float score = 0.f;
-    const uint4* gate16 = static_cast<const uint4*>(a.gate) + (a.gate_kind == SPA_GATE_IMAGE ? (long long)(t / a.N) * a.Q : at);
-    const bool gates = a.gate_kind == SPA_GATE_IMAGE || a.gate_kind == SPA_GATE_TOKEN;
-#pragma unroll
-    for (int k = 0; k < kCh; ++k) {
-      const int q = t0 + G * k;
-      xr[k] = zv[k] = gr[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (q < a.Q) {
-        xr[k] = ld_stream16(a.x + at + q);
-        if (has) {
-          zv[k] = ld_stream16(a.z + zat + q);
-          if (gates) gr[k] = gate16[q];
-        }
-      }
-    }
-    if (has && a.gate_kind == SPA_GATE_SCORE) score = sigmoid(static_cast<const float*>(a.gate)[t]);
-    float v[kCh][E], m1 = 0.f, r1 = 0.f;
-    if (has) {
-#pragma unroll
-      for (int k = 0; k < kCh; ++k) Vec16<T>::to_float(zv[k], v[k]);
-      statistics(v, m1, r1);
-    }
-#pragma unroll
-    for (int k = 0; k < kCh; ++k) {
-      const int q = t0 + G * k;
-      float x[E];
-      Vec16<T>::to_float(xr[k], x);
-      if (has && q < a.Q) {
-        float gp[E], bp[E], sc[E], g[E];
-        chunk_or<T>(a.g_post, q, 1.f, gp);
-        chunk_or<T>(a.b_post, q, 0.f, bp);
-        chunk_or<T>(a.scale, q, 1.f, sc);
-        Vec16<T>::to_float(gr[k], g);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float w = gates ? g[e] : (a.gate_kind == SPA_GATE_SCORE ? score : 1.f);
-          x[e] = fmaf(fmaf((v[k][e] - m1) * r1, gp[e], bp[e]), sc[e] * w, x[e]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = x[e];
-      if (q < a.Q) a.out_y[at + q] = has ? Vec16<T>::from_float(x) : xr[k];
-    }
-    float m2 = 0.f, r2 = 0.f;
-    if (a.out_n != nullptr) {
-      statistics(v, m2, r2);
+  extern __shared__ __align__(16) uint8_t ring_s[];
+  Ring<kFwdArrays<kGate>, kCh, kFwdDepth, threads_of(W, false)> ring{ring_s, 0};
+  auto row_of = [&](int t) { return a.z_row != nullptr && t < a.rows ? ld_dep(a.z_row + t) : t; };
+  auto has_row = [&](int zr) { return zr >= 0 && zr < a.z_rows; };
+  auto fetch = [&](int t, int zr) {
+    if (t < a.rows) {
+      const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
+      const uint4* gate16 = static_cast<const uint4*>(a.gate) + (kGate == SPA_GATE_IMAGE ? (long long)(t / a.N) * a.Q : at);
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
         const int q = t0 + G * k;
         if (q < a.Q) {
-          float gp[E], bp[E], o[E];
-          chunk_or<T>(a.g_pre, q, 1.f, gp);
-          chunk_or<T>(a.b_pre, q, 0.f, bp);
+          ring.copy(0, k, a.x + at + q);
+          if (has_row(zr)) {
+            ring.copy(1, k, a.z + zat + q);
+            if (kGateRows<kGate>) ring.copy(kGateRows<kGate> ? 2 : 0, k, gate16 + q);
+          }
+        }
+      }
+      if (kGate == SPA_GATE_SCORE && sum.lane == 0) ring.copy_scalar(0, static_cast<const float*>(a.gate) + t);
+    }
+    cp_async_commit();
+  };
+  const int step = gridDim.x * groups_of(W, false);
+  int t = blockIdx.x * groups_of(W, false) + grp;
+  int zr[kFwdDepth + 1];  // rows of z of the tokens on their way, and of one more
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = fmaf((v[k][e] - m2) * r2, gp[e], bp[e]);
-          a.out_n[at + q] = Vec16<T>::from_float(o);
+  for (int i = 0; i <= kFwdDepth; ++i) zr[i] = row_of(t + i * step);
+#pragma unroll
+  for (int i = 0; i < kFwdDepth; ++i) {
+    fetch(t + i * step, zr[i]);
+    ring.next();
+  }
+  for (; t < a.rows; t += step) {
+    const bool has = has_row(zr[0]);
+    cp_async_wait<kFwdDepth - 1>();
+    __syncwarp();
+    uint4 xr[kCh], zv[kCh], gr[kCh];
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int k = 0; k < kCh; ++k) {
+      const bool in = t0 + G * k < a.Q;
+      xr[k] = in ? ring.get(0, k) : zero;
+      zv[k] = in && has ? ring.get(1, k) : zero;
+      gr[k] = in && has && kGateRows<kGate> ? ring.get(kGateRows<kGate> ? 2 : 0, k) : zero;
+    }
+    const float score = kGate == SPA_GATE_SCORE ? ring.scalars()[0] : 0.f;
+    __syncwarp();
+    fetch(t + kFwdDepth * step, zr[kFwdDepth]);
+    ring.next();
+#pragma unroll
+    for (int i = 0; i < kFwdDepth; ++i) zr[i] = zr[i + 1];
+    zr[kFwdDepth] = row_of(t + (kFwdDepth + 1) * step);
+    uint64_t v[kCh][P];
+    float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
+    const long long at = (long long)t * a.Q;
+    if (has) {
+#pragma unroll
+      for (int k = 0; k < kCh; ++k) to_pairs(zv[k], v[k]);
+      statistics(v, m1, r1);
+      const uint64_t r = both(r1), m = both(-m1 * r1), w = both(kGate == SPA_GATE_SCORE ? sigmoid(score) : 1.f);
+#pragma unroll
+      for (int k = 0; k < kCh; ++k) {
+        uint64_t x[P], g[P];
+        to_pairs(xr[k], x);
+        if (kGateRows<kGate>) to_pairs(gr[k], g);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const uint64_t b = fma2(fma2(v[k][i], r, m), cw[k][i], cb[k][i]);
+          v[k][i] = kGate == SPA_GATE_NONE ? add2(b, x[i]) : fma2(b, kGateRows<kGate> ? g[i] : w, x[i]);
+        }
+        if (t0 + G * k < a.Q) a.out_y[at + t0 + G * k] = from_pairs(v[k]);
+        else {
+#pragma unroll
+          for (int i = 0; i < P; ++i) v[k][i] = 0ull;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kCh; ++k) {
+        to_pairs(xr[k], v[k]);
+        if (t0 + G * k < a.Q) a.out_y[at + t0 + G * k] = xr[k];
+      }
+    }
+    if (a.out_n != nullptr) {
+      statistics(v, m2, r2);
+      const uint64_t r = both(r2), m = both(-m2 * r2);
+#pragma unroll
+      for (int k = 0; k < kCh; ++k) {
+        if (t0 + G * k < a.Q) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) v[k][i] = fma2(fma2(v[k][i], r, m), cp[k][i], bp[k][i]);
+          a.out_n[at + t0 + G * k] = from_pairs(v[k]);
         }
       }
     }
@@ -179,24 +325,34 @@ __global__ void __launch_bounds__(kThreads<W>) sandwich_fwd_kernel(const Args a)
   }
 }
 
-// Rows are taken in units: with a gate per image a unit is a split of one image's rows, so that its sums A_b and B_b leave the CTA
-// at its end; otherwise a CTA has one unit, its share of all rows.
-template <typename T, int W, int kCh>
-__global__ void __launch_bounds__(kThreads<W>) sandwich_bwd_kernel(const Args a) {
+template <int kGate> constexpr int kBwdArrays = kGate == SPA_GATE_TOKEN ? 5 : 4;
+template <int kCh> constexpr int kBwdDepth = kCh == 1 ? 3 : 2;
+
+// A CTA has a share of the rows, one behind the other.  With a gate per image the sums A_b and B_b leave it at the end of each image
+// or share: the line of image b from CTA c is line b + c, since one of the two goes up from each to the next.
+template <typename T, int W, int kCh, int kGate>
+__global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(const Args a) {
   pdl_entry();
-  constexpr int E = Vec16<T>::kElems, G = 32 * W, kG = kGroups<W>;
-  extern __shared__ __align__(16) float acc_s[];  // [kG][2][C], and behind it, with a gate per image, [2][C]: sum of gate_b A_b, of gate_b B_b
-  __shared__ float red[kG * 4 * W];
+  constexpr int P = kPairs<T>, G = 32 * W, kG = groups_of(W, true);
+  constexpr bool kImage = kGate == SPA_GATE_IMAGE;
+  constexpr int kDepth = kBwdDepth<kCh>;
+  using Rows = Ring<kBwdArrays<kGate>, kCh, kDepth, threads_of(W, true)>;
+  // the ring, and in its place, when it is empty, [kG][2][C] sums; behind them, with a gate per image, [2][C]: sum of gate_b A_b,
+  // of gate_b B_b
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* acc_s = reinterpret_cast<float*>(smem);
+  __shared__ __align__(16) float red[kG * 8 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  GroupSum<W> sum{red + grp * 4 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
+  GroupSum<W> sum{red + grp * 8 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
   const float inv_c = 1.f / a.C;
-  const bool layer = a.kind == SPA_NORM_LAYER, per_image = a.gate_kind == SPA_GATE_IMAGE;
-  float sA[kCh][E] = {}, sB[kCh][E] = {}, sG[kCh][E] = {}, sN[kCh][E] = {};
-  float* run = acc_s + (size_t)kG * 2 * a.C;
-  if (per_image)
-    for (int c = threadIdx.x; c < 2 * a.C; c += kThreads<W>) run[c] = 0.f;  // each thread its own, also below
+  const bool layer = a.kind == SPA_NORM_LAYER;
+  uint64_t sA[kCh][P] = {}, sB[kCh][P] = {}, sG[kCh][P] = {}, sN[kCh][P] = {};
+  const int acc_bytes = kG * 2 * a.C * 4;
+  float* run = reinterpret_cast<float*>(smem + (acc_bytes > Rows::kBytes ? acc_bytes : Rows::kBytes));
+  if (kImage)
+    for (int c = threadIdx.x; c < 2 * a.C; c += threads_of(W, true)) run[c] = 0.f;
   // two running sums of every group, added up in the order of the groups, to out(c, first, second)
-  auto join = [&](const float (&u)[kCh][E], const float (&w)[kCh][E], auto out) {
+  auto join = [&](const uint64_t (&u)[kCh][P], const uint64_t (&w)[kCh][P], auto out) {
     __syncthreads();
     float* mine = acc_s + grp * 2 * a.C;
 #pragma unroll
@@ -204,166 +360,225 @@ __global__ void __launch_bounds__(kThreads<W>) sandwich_bwd_kernel(const Args a)
       const int q = t0 + G * k;
       if (q < a.Q) {
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-          *reinterpret_cast<float4*>(mine + q * E + e) = make_float4(u[k][e], u[k][e + 1], u[k][e + 2], u[k][e + 3]);
-          *reinterpret_cast<float4*>(mine + a.C + q * E + e) = make_float4(w[k][e], w[k][e + 1], w[k][e + 2], w[k][e + 3]);
+        for (int i = 0; i < P; i += 2) {
+          *reinterpret_cast<ulonglong2*>(mine + (q * P + i) * 2) = make_ulonglong2(u[k][i], u[k][i + 1]);
+          *reinterpret_cast<ulonglong2*>(mine + a.C + (q * P + i) * 2) = make_ulonglong2(w[k][i], w[k][i + 1]);
         }
       }
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < a.C; c += kThreads<W>) {
+    for (int c = threadIdx.x; c < a.C; c += threads_of(W, true)) {
       float s = 0.f, r = 0.f;
 #pragma unroll
       for (int g = 0; g < kG; ++g) { s += acc_s[g * 2 * a.C + c]; r += acc_s[g * 2 * a.C + a.C + c]; }
       out(c, s, r);
     }
   };
-  for (int unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
-    int first = unit * kG + grp, step = a.units * kG, end = a.rows, image = 0;
-    if (per_image) {
-      image = unit / a.splits;
-      const int split = unit - image * a.splits, per = (a.N + a.splits - 1) / a.splits;
-      first = image * a.N + split * per + grp;
-      step = kG;
-      end = image * a.N + (split * per + per < a.N ? split * per + per : a.N);
-    }
-    for (int t = first; t < end; t += step) {
-      int zr = t;
-      if (a.z_row != nullptr) zr = ld_dep(a.z_row + t);
-      const bool has = zr >= 0 && zr < a.z_rows;
-      const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
-      const uint4* gate16 = static_cast<const uint4*>(a.gate) + (per_image ? (long long)image * a.Q : at);
-      const bool gates = per_image || a.gate_kind == SPA_GATE_TOKEN;
-      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-      uint4 nr[kCh], dr[kCh], yr[kCh], zv[kCh], gr[kCh];
+  // gz = d gate cw; a / gate = cw zh + cb (for the gradient of a gate that is not per image)
+  uint64_t cp[kCh][P], cw[kCh][P], cb[kCh][P];
+#pragma unroll
+  for (int k = 0; k < kCh; ++k) {
+    const int q = t0 + G * k;
+    const bool in = q < a.Q;
+    uint64_t sc[P];
+    param<T>(a.scale, q, in, 1.f, sc);
+    param<T>(a.g_post, q, in, 1.f, cw[k]);
+    param<T>(a.g_pre, q, in, 1.f, cp[k]);
+    param<T>(a.b_post, q, in, 0.f, cb[k]);
+#pragma unroll
+    for (int i = 0; i < P; ++i) { cw[k][i] = mul2(cw[k][i], sc[i]); cb[k][i] = mul2(cb[k][i], sc[i]); }
+  }
+  struct Row { uint4 n[kCh], y[kCh], d[kCh], z[kCh], g[kGate == SPA_GATE_TOKEN ? kCh : 1]; float m1, r1, m2, r2, score; int zr; };
+  Rows ring{smem, 0};
+  auto has_row = [&](int zr) { return zr >= 0 && zr < a.z_rows; };
+  const int share = blockIdx.x * a.rows_per_cta, share_end = share + a.rows_per_cta < a.rows ? share + a.rows_per_cta : a.rows;
+  for (int begin = share, end; begin < share_end; begin = end) {
+    const int image = kImage ? begin / a.N : 0;
+    end = kImage && (image + 1) * a.N < share_end ? (image + 1) * a.N : share_end;
+    uint64_t cg[kCh][P];  // gate per image: cw times it
+    if (kImage) {
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
-        const int q = t0 + G * k;
-        const bool in = q < a.Q;
-        nr[k] = in && a.dn != nullptr ? ld_stream16(a.dn + at + q) : zero;
-        yr[k] = in && a.dn != nullptr ? ld_stream16(a.y + at + q) : zero;
-        dr[k] = in && a.dy != nullptr ? ld_stream16(a.dy + at + q) : zero;
-        zv[k] = in && has ? ld_stream16(a.z + zat + q) : zero;
-        gr[k] = in && has && gates ? gate16[q] : zero;
+        param<T>(static_cast<const uint4*>(a.gate) + (long long)image * a.Q, t0 + G * k, t0 + G * k < a.Q, 0.f, cg[k]);
+#pragma unroll
+        for (int i = 0; i < P; ++i) cg[k][i] = mul2(cg[k][i], cw[k][i]);
       }
-      const float m1 = a.stats[t], r1 = a.stats[a.rows + t];
-      float m2 = 0.f, r2 = 0.f, score = 1.f;
-      if (a.dn != nullptr) { m2 = a.stats[2 * a.rows + t]; r2 = a.stats[3 * a.rows + t]; }
-      if (a.gate_kind == SPA_GATE_SCORE) score = sigmoid(static_cast<const float*>(a.gate)[t]);
+    }
+    auto row_of = [&](int t) { return a.z_row != nullptr && t < end ? ld_dep(a.z_row + t) : t; };
+    auto fetch = [&](int t, int zr) {
+      if (t < end) {
+        const bool has = has_row(zr);
+        const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
+#pragma unroll
+        for (int k = 0; k < kCh; ++k) {
+          const int q = t0 + G * k;
+          if (q < a.Q) {
+            if (a.dn != nullptr) {
+              ring.copy(0, k, a.dn + at + q);
+              ring.copy(1, k, a.y + at + q);
+            }
+            if (a.dy != nullptr) ring.copy(2, k, a.dy + at + q);
+            if (has) {
+              ring.copy(3, k, a.z + zat + q);
+              if (kGate == SPA_GATE_TOKEN) ring.copy(kGate == SPA_GATE_TOKEN ? 4 : 0, k, static_cast<const uint4*>(a.gate) + at + q);
+            }
+          }
+        }
+        if (sum.lane < 4) ring.copy_scalar(sum.lane, a.stats + (long long)sum.lane * a.rows + t);
+        if (kGate == SPA_GATE_SCORE && sum.lane == 4) ring.copy_scalar(4, static_cast<const float*>(a.gate) + t);
+      }
+      cp_async_commit();
+    };
+    int t = begin + grp, zr[kDepth + 1];  // rows of z of the tokens on their way, and of one more
+#pragma unroll
+    for (int i = 0; i <= kDepth; ++i) zr[i] = row_of(t + i * kG);
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) {
+      fetch(t + i * kG, zr[i]);
+      ring.next();
+    }
+    for (; t < end; t += kG) {
+      cp_async_wait<kDepth - 1>();
+      __syncwarp();
+      Row cur;
+      {
+        const bool has = has_row(zr[0]);
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        cur.zr = has ? zr[0] : -1;
+#pragma unroll
+        for (int k = 0; k < kCh; ++k) {
+          const bool in = t0 + G * k < a.Q;
+          cur.n[k] = in && a.dn != nullptr ? ring.get(0, k) : zero;
+          cur.y[k] = in && a.dn != nullptr ? ring.get(1, k) : zero;
+          cur.d[k] = in && a.dy != nullptr ? ring.get(2, k) : zero;
+          cur.z[k] = in && has ? ring.get(3, k) : zero;
+          if constexpr (kGate == SPA_GATE_TOKEN) cur.g[k] = in && has ? ring.get(4, k) : zero;
+        }
+        const float* sc = ring.scalars();
+        cur.m1 = sc[0];
+        cur.r1 = sc[1];
+        cur.m2 = sc[2];
+        cur.r2 = sc[3];
+        cur.score = kGate == SPA_GATE_SCORE ? sc[4] : 0.f;
+      }
+      __syncwarp();
+      fetch(t + kDepth * kG, zr[kDepth]);
+      ring.next();
+#pragma unroll
+      for (int i = 0; i < kDepth; ++i) zr[i] = zr[i + 1];
+      zr[kDepth] = row_of(t + (kDepth + 1) * kG);
+      const long long at = (long long)t * a.Q, zat = (long long)cur.zr * a.Q;
+      const bool has = cur.zr >= 0;
       // ---- through the norm behind the sum: d, the gradient of y
-      float d[kCh][E];
-      float s1 = 0.f, s2 = 0.f;
+      uint64_t d[kCh][P];
       if (a.dn != nullptr) {
+        const uint64_t r = both(cur.r2), m = both(-cur.m2 * cur.r2);
+        uint64_t s1 = 0ull, s2 = 0ull, yh[kCh][P];
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
-          const int q = t0 + G * k;
-          if (q < a.Q) {
-            float n[E], y[E], gp[E];
-            Vec16<T>::to_float(nr[k], n);
-            Vec16<T>::to_float(yr[k], y);
-            chunk_or<T>(a.g_pre, q, 1.f, gp);
+          uint64_t n[P];
+          to_pairs(cur.n[k], n);
+          to_pairs(cur.y[k], yh[k]);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float yh = (y[e] - m2) * r2, g = n[e] * gp[e];
-              s1 += g;
-              s2 = fmaf(g, yh, s2);
-              sG[k][e] = fmaf(n[e], yh, sG[k][e]);
-              sN[k][e] += n[e];
-            }
+          for (int i = 0; i < P; ++i) {  // chunks past the end: n is zero
+            yh[k][i] = fma2(yh[k][i], r, m);
+            sG[k][i] = fma2(n[i], yh[k][i], sG[k][i]);
+            sN[k][i] = add2(sN[k][i], n[i]);
+            d[k][i] = mul2(n[i], cp[k][i]);
+            s1 = add2(s1, d[k][i]);
+            s2 = fma2(d[k][i], yh[k][i], s2);
           }
         }
-        sum(s1, s2);
-        s1 = layer ? s1 * inv_c : 0.f;
-        s2 *= inv_c;
-      }
-      float u1 = 0.f, u2 = 0.f;
+        float s[2] = {sum_of(s1), sum_of(s2)};
+        sum(s);
+        // d = dy + (g - mean g - yh mean(g yh)) / deviation
+        const uint64_t a1 = both(layer ? -s[0] * inv_c * cur.r2 : 0.f), a2 = both(-s[1] * inv_c * cur.r2);
 #pragma unroll
-      for (int k = 0; k < kCh; ++k) {
-        const int q = t0 + G * k;
-        Vec16<T>::to_float(dr[k], d[k]);
-        if (q < a.Q) {
-          if (a.dn != nullptr) {
-            float n[E], y[E], gp[E];
-            Vec16<T>::to_float(nr[k], n);
-            Vec16<T>::to_float(yr[k], y);
-            chunk_or<T>(a.g_pre, q, 1.f, gp);
+        for (int k = 0; k < kCh; ++k) {
+          uint64_t y[P];
+          to_pairs(cur.d[k], y);
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[k][e] += (n[e] * gp[e] - s1 - (y[e] - m2) * r2 * s2) * r2;
-          }
-          a.dx[at + q] = Vec16<T>::from_float(d[k]);
-          if (has) {
-            float z[E], g[E], gp[E], sc[E], bp[E];
-            Vec16<T>::to_float(zv[k], z);
-            Vec16<T>::to_float(gr[k], g);
-            chunk_or<T>(a.g_post, q, 1.f, gp);
-            chunk_or<T>(a.scale, q, 1.f, sc);
-            float o[E];
-            if (a.gate_kind == SPA_GATE_TOKEN) chunk_or<T>(a.b_post, q, 0.f, bp);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float zh = (z[e] - m1) * r1, w = gates ? g[e] : score;
-              const float dw = per_image ? d[k][e] : d[k][e] * w;
-              sA[k][e] = fmaf(dw, zh, sA[k][e]);
-              sB[k][e] += dw;
-              const float gz = d[k][e] * w * sc[e] * gp[e];
-              u1 += gz;
-              u2 = fmaf(gz, zh, u2);
-              if (a.gate_kind == SPA_GATE_TOKEN) o[e] = d[k][e] * sc[e] * fmaf(zh, gp[e], bp[e]);
-            }
-            if (a.gate_kind == SPA_GATE_TOKEN) {
-              if (a.dgate != nullptr) static_cast<uint4*>(a.dgate)[at + q] = Vec16<T>::from_float(o);
-            }
-          } else if (a.gate_kind == SPA_GATE_TOKEN && a.dgate != nullptr) {
-            static_cast<uint4*>(a.dgate)[at + q] = zero;
-          }
+          for (int i = 0; i < P; ++i) d[k][i] = add2(y[i], fma2(d[k][i], r, fma2(yh[k][i], a2, a1)));
         }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kCh; ++k) to_pairs(cur.d[k], d[k]);
       }
+#pragma unroll
+      for (int k = 0; k < kCh; ++k)
+        if (t0 + G * k < a.Q) a.dx[at + t0 + G * k] = from_pairs(d[k]);
       if (has) {
-        // score: dgate = score (1 - score) sum d scale (g_post zh + b_post)
-        if (a.gate_kind == SPA_GATE_SCORE && a.dgate != nullptr) {
-          float v = 0.f, none = 0.f;
-#pragma unroll
-          for (int k = 0; k < kCh; ++k) {
-            const int q = t0 + G * k;
-            if (q < a.Q) {
-              float z[E], gp[E], sc[E], bp[E];
-              Vec16<T>::to_float(zv[k], z);
-              chunk_or<T>(a.g_post, q, 1.f, gp);
-              chunk_or<T>(a.scale, q, 1.f, sc);
-              chunk_or<T>(a.b_post, q, 0.f, bp);
-#pragma unroll
-              for (int e = 0; e < E; ++e) v = fmaf(d[k][e] * sc[e], fmaf((z[e] - m1) * r1, gp[e], bp[e]), v);
-            }
-          }
-          sum(v, none);
-          if (t0 == 0) static_cast<float*>(a.dgate)[t] = v * score * (1.f - score);
-        }
-        sum(u1, u2);
-        u1 = layer ? u1 * inv_c : 0.f;
-        u2 *= inv_c;
+        const float score = kGate == SPA_GATE_SCORE ? sigmoid(cur.score) : 1.f;
+        const uint64_t r = both(cur.r1), m = both(-cur.m1 * cur.r1), w = both(score);
+        uint64_t u1 = 0ull, u2 = 0ull, u3 = 0ull, zh[kCh][P];
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
-          const int q = t0 + G * k;
-          if (q < a.Q) {
-            float z[E], g[E], gp[E], sc[E], o[E];
-            Vec16<T>::to_float(zv[k], z);
-            Vec16<T>::to_float(gr[k], g);
-            chunk_or<T>(a.g_post, q, 1.f, gp);
-            chunk_or<T>(a.scale, q, 1.f, sc);
+          const bool in = t0 + G * k < a.Q;
+          uint64_t g[P];
+          to_pairs(cur.z[k], zh[k]);
+          if constexpr (kGate == SPA_GATE_TOKEN) to_pairs(cur.g[k], g);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float w = gates ? g[e] : score;
-              o[e] = (d[k][e] * w * sc[e] * gp[e] - u1 - (z[e] - m1) * r1 * u2) * r1;
+          for (int i = 0; i < P; ++i) {
+            if (!in) d[k][i] = 0ull;
+            zh[k][i] = fma2(zh[k][i], r, m);
+            if (kGate == SPA_GATE_SCORE) u3 = fma2(d[k][i], fma2(zh[k][i], cw[k][i], cb[k][i]), u3);
+            if constexpr (kGate == SPA_GATE_TOKEN) {
+              const uint64_t dg = mul2(d[k][i], fma2(zh[k][i], cw[k][i], cb[k][i]));
+              d[k][i] = mul2(d[k][i], g[i]);
+              g[i] = dg;
             }
-            a.dz[zat + q] = Vec16<T>::from_float(o);
+            if (kGate == SPA_GATE_SCORE) d[k][i] = mul2(d[k][i], w);
+            sA[k][i] = fma2(d[k][i], zh[k][i], sA[k][i]);
+            sB[k][i] = add2(sB[k][i], d[k][i]);
+            d[k][i] = mul2(d[k][i], kImage ? cg[k][i] : cw[k][i]);  // gz
+            u1 = add2(u1, d[k][i]);
+            u2 = fma2(d[k][i], zh[k][i], u2);
+          }
+          if constexpr (kGate == SPA_GATE_TOKEN) {
+            if (in && a.dgate != nullptr) {
+              if (a.gate_f32) {
+#pragma unroll
+                for (int i = 0; i < P; i += 2)
+                  static_cast<ulonglong2*>(a.dgate)[((at + t0 + G * k) * P + i) / 2] = make_ulonglong2(g[i], g[i + 1]);
+              } else {
+                static_cast<uint4*>(a.dgate)[at + t0 + G * k] = from_pairs(g);
+              }
+            }
           }
         }
-      } else if (a.gate_kind == SPA_GATE_SCORE && a.dgate != nullptr && t0 == 0) {
-        static_cast<float*>(a.dgate)[t] = 0.f;
+        float s[kGate == SPA_GATE_SCORE ? 3 : 2];
+        s[0] = sum_of(u1);
+        s[1] = sum_of(u2);
+        if constexpr (kGate == SPA_GATE_SCORE) s[2] = sum_of(u3);
+        sum(s);
+        if constexpr (kGate == SPA_GATE_SCORE) {
+          if (t0 == 0 && a.dgate != nullptr) static_cast<float*>(a.dgate)[t] = s[2] * score * (1.f - score);
+        }
+        const uint64_t a1 = both(layer ? -s[0] * inv_c * cur.r1 : 0.f), a2 = both(-s[1] * inv_c * cur.r1);
+#pragma unroll
+        for (int k = 0; k < kCh; ++k) {
+          if (t0 + G * k < a.Q) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) d[k][i] = fma2(d[k][i], r, fma2(zh[k][i], a2, a1));
+            a.dz[zat + t0 + G * k] = from_pairs(d[k]);
+          }
+        }
+      } else if (a.dgate != nullptr) {
+        if (kGate == SPA_GATE_SCORE && t0 == 0) static_cast<float*>(a.dgate)[t] = 0.f;
+        if (kGate == SPA_GATE_TOKEN) {
+#pragma unroll
+          for (int k = 0; k < kCh; ++k)
+            if (t0 + G * k < a.Q) {
+#pragma unroll
+              for (int i = 0; i < (a.gate_f32 ? P / 2 : 1); ++i)
+                static_cast<uint4*>(a.dgate)[(at + t0 + G * k) * (a.gate_f32 ? P / 2 : 1) + i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
       }
     }
-    if (per_image) {
-      float* to = a.part_gate + (size_t)unit * 2 * a.C;
+    cp_async_wait<0>();
+    if (kImage) {  // (join starts with a barrier: the ring is empty)
+      float* to = a.part_gate + (size_t)(blockIdx.x + image) * 2 * a.C;
       const T* g = static_cast<const T*>(a.gate) + (size_t)image * a.C;
       join(sA, sB, [&](int c, float A, float B) {
         to[c] = A;
@@ -375,13 +590,14 @@ __global__ void __launch_bounds__(kThreads<W>) sandwich_bwd_kernel(const Args a)
 #pragma unroll
       for (int k = 0; k < kCh; ++k)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sA[k][e] = sB[k][e] = 0.f;
+        for (int i = 0; i < P; ++i) sA[k][i] = sB[k][i] = 0ull;
+      __syncthreads();  // the sums' memory becomes the ring again
     }
   }
   float* to = a.part + (size_t)blockIdx.x * kSums * a.C;
-  if (per_image) {
+  if (kImage) {
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.C; c += kThreads<W>) to[c] = run[c];
+    for (int c = threadIdx.x; c < 2 * a.C; c += threads_of(W, true)) to[c] = run[c];
   } else {
     join(sA, sB, [&](int c, float A, float B) { to[c] = A; to[a.C + c] = B; });
   }
@@ -389,19 +605,21 @@ __global__ void __launch_bounds__(kThreads<W>) sandwich_bwd_kernel(const Args a)
 }
 
 // The parameters' gradients from the CTAs' sums, added up in their order: 32 channels a block, blockIdx.x = 0; and with a gate per
-// image, blockIdx.x = 1 + image, its gradient from the units of its rows.
+// image, blockIdx.x = 1 + image, its gradient from its lines.
 constexpr int kJoinLanes = 16;
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinLanes)
-sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int splits, int C, const T* scale, const T* g_post,
+sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int N, int rows_per_cta, int C, const T* scale, const T* g_post,
                      const T* b_post, float* __restrict__ dgate, float* __restrict__ dscale, float* __restrict__ dg_post,
                      float* __restrict__ db_post, float* __restrict__ dg_pre, float* __restrict__ db_pre) {
   pdl_entry();
   __shared__ float s[kSums][kJoinLanes][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.y * 32 + x;
   const bool images = blockIdx.x > 0;
-  const int lines = images ? splits : ctas, sums = images ? 2 : kSums;
-  const float* from = images ? part_gate + (size_t)(blockIdx.x - 1) * splits * 2 * C : part;
+  // an image's lines: those of the CTAs whose rows it has a part of
+  const int b = blockIdx.x - 1, c0 = images ? (int)((long long)b * N / rows_per_cta) : 0;
+  const int lines = images ? (int)(((long long)b * N + N - 1) / rows_per_cta) - c0 + 1 : ctas, sums = images ? 2 : kSums;
+  const float* from = images ? part_gate + (size_t)(b + c0) * 2 * C : part;
   float v[kSums] = {};
   if (c < C) {
 #pragma unroll 4
@@ -435,30 +653,23 @@ sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int sp
 
 int chunks_of(const spa_params& p) { return p.C / (p.dtype == SPA_F32 ? 4 : 8); }
 
-// Warps to a row: as few as leave a thread `most` chunks or fewer
-int warps_of(int Q, int most) {
-  int w = 1;
-  while (w < 16 && Q > 32 * w * most) w *= 2;
-  return w;
+// Warps to a row: as few as leave a thread one chunk, up to sixteen
+int warps_of(int Q) {
+  for (int w : {1, 2, 3, 4, 6, 8, 12})
+    if (Q <= 32 * w) return w;
+  return 16;
 }
 
-// Units of rows: per image so many splits that the CTAs of the grid have one each; otherwise one per CTA.
-struct Plan { int ctas, units, splits, warps; };
+// The backward's shares of rows.  Images of one token: their gate is one per token, and no sum leaves a CTA for it.
+struct Plan { int ctas, rows_per_cta, gate_kind; };
 Plan bwd_plan(const spa_params& p, const spa_sandwich& s) {
+  const int groups = groups_of(warps_of(chunks_of(p)), true), rows = p.B * p.N;
+  int ctas = (rows + groups - 1) / groups;
+  ctas = ctas < 1 ? 1 : (ctas > kNumSMs ? kNumSMs : ctas);
   Plan r;
-  r.warps = warps_of(chunks_of(p), 2);
-  const int groups = r.warps == 16 ? 1 : 8 / r.warps, most = kNumSMs * (r.warps == 16 ? 1 : 2), rows = p.B * p.N;
-  if (s.gate_kind == SPA_GATE_IMAGE) {
-    r.splits = p.B >= most || p.B == 0 ? 1 : most / p.B;
-    const int useful = (p.N + groups - 1) / groups;
-    if (r.splits > useful) r.splits = useful;
-    r.units = p.B * r.splits;
-  } else {
-    r.splits = 1;
-    r.units = (rows + groups - 1) / groups;
-    if (r.units > most) r.units = most;
-  }
-  r.ctas = r.units < most ? r.units : most;
+  r.rows_per_cta = rows > 0 ? (rows + ctas - 1) / ctas : 1;
+  r.ctas = rows > 0 ? (rows + r.rows_per_cta - 1) / r.rows_per_cta : 1;
+  r.gate_kind = s.gate_kind == SPA_GATE_IMAGE && p.N == 1 ? (int)SPA_GATE_TOKEN : s.gate_kind;
   return r;
 }
 
@@ -478,29 +689,64 @@ Args args_of(const spa_params& p, const spa_sandwich& s, const void* z, const in
   a.C = p.C;
   a.z_rows = z_row != nullptr ? p.capacity : p.B * p.N;
   a.kind = s.kind;
-  a.gate_kind = s.gate_kind;
   a.eps = s.eps;
   return a;
 }
 
-template <typename T, int W, int kCh> int fwd_launch(const Args& a, cudaStream_t st) {
-  const int need = (a.rows + kGroups<W> - 1) / kGroups<W>, most = kNumSMs * (W == 16 ? 3 : 6);
-  launch_pdl(sandwich_fwd_kernel<T, W, kCh>, need < most ? need : most, kThreads<W>, 0, st, a);
+template <typename T, int W, int kCh, int kGate> int fwd_launch(const Args& a, cudaStream_t st) {
+  const int need = (a.rows + groups_of(W, false) - 1) / groups_of(W, false), most = kNumSMs * (1024 / threads_of(W, false));
+  auto kern = sandwich_fwd_kernel<T, W, kCh, kGate>;
+  constexpr int kSmem = Ring<kFwdArrays<kGate>, kCh, kFwdDepth, threads_of(W, false)>::kBytes;
+  static DeviceOnce attr;
+  cudaError_t e = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+  if (e != cudaSuccess) { set_cuda_error(e, "sandwich_fwd_kernel"); return SPA_ERR_CUDA; }
+  launch_pdl(kern, need < most ? need : most, threads_of(W, false), kSmem, st, a);
   SPA_CUDA_CHECK_LAUNCH("sandwich_fwd_kernel");
   return SPA_OK;
 }
 
-template <typename T, int W, int kCh> int bwd_launch(const Args& a, const Plan& pl, cudaStream_t st) {
-  auto kern = sandwich_bwd_kernel<T, W, kCh>;
-  const size_t smem = (size_t)(kGroups<W> + 1) * 2 * a.C * sizeof(float);
-  constexpr int kMost = (kGroups<W> + 1) * 2 * 32 * W * kCh * Vec16<T>::kElems * (int)sizeof(float);
+template <typename T, int W, int kCh, int kGate> int bwd_launch(const Args& a, const Plan& pl, cudaStream_t st) {
+  auto kern = sandwich_bwd_kernel<T, W, kCh, kGate>;
+  constexpr int kRing = Ring<kBwdArrays<kGate>, kCh, kBwdDepth<kCh>, threads_of(W, true)>::kBytes;
+  auto bytes = [](int channels) {
+    const int acc = groups_of(W, true) * 2 * channels * (int)sizeof(float);
+    return (acc > kRing ? acc : kRing) + (kGate == SPA_GATE_IMAGE ? 2 * channels * (int)sizeof(float) : 0);
+  };
+  const int smem = bytes(a.C), kMost = bytes(32 * W * kCh * Vec16<T>::kElems);
   static DeviceOnce attr;
   cudaError_t e = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); });
   if (e != cudaSuccess) { set_cuda_error(e, "sandwich_bwd_kernel"); return SPA_ERR_CUDA; }
-  launch_pdl(kern, pl.ctas, kThreads<W>, smem, st, a);
+  launch_pdl(kern, pl.ctas, threads_of(W, true), smem, st, a);
   SPA_CUDA_CHECK_LAUNCH("sandwich_bwd_kernel");
   return SPA_OK;
 }
+
+// WHICH<T, warps, chunks of a thread, gate>
+#define SPA_BY_WARPS(WHICH, T, GATE, ...)                          \
+  switch (warps_of(a.Q)) {                                         \
+    case 1: return WHICH<T, 1, 1, GATE>(__VA_ARGS__);              \
+    case 2: return WHICH<T, 2, 1, GATE>(__VA_ARGS__);              \
+    case 3: return WHICH<T, 3, 1, GATE>(__VA_ARGS__);              \
+    case 4: return WHICH<T, 4, 1, GATE>(__VA_ARGS__);              \
+    case 6: return WHICH<T, 6, 1, GATE>(__VA_ARGS__);              \
+    case 8: return WHICH<T, 8, 1, GATE>(__VA_ARGS__);              \
+    case 12: return WHICH<T, 12, 1, GATE>(__VA_ARGS__);            \
+    default:                                                       \
+      if (a.Q <= 512) return WHICH<T, 16, 1, GATE>(__VA_ARGS__);   \
+      return WHICH<T, 16, 2, GATE>(__VA_ARGS__);                   \
+  }
+template <typename T, int kGate> int fwd_by_warps(const Args& a, cudaStream_t st) { SPA_BY_WARPS(fwd_launch, T, kGate, a, st) }
+template <typename T, int kGate> int bwd_by_warps(const Args& a, const Plan& pl, cudaStream_t st) { SPA_BY_WARPS(bwd_launch, T, kGate, a, pl, st) }
+#undef SPA_BY_WARPS
+#define SPA_BY_GATE(KIND, WHICH, ...)                                                                             \
+  (p.dtype == SPA_F32 ? ((KIND) == SPA_GATE_NONE    ? WHICH<float, SPA_GATE_NONE>(__VA_ARGS__)         \
+                         : (KIND) == SPA_GATE_SCORE ? WHICH<float, SPA_GATE_SCORE>(__VA_ARGS__)        \
+                         : (KIND) == SPA_GATE_IMAGE ? WHICH<float, SPA_GATE_IMAGE>(__VA_ARGS__)        \
+                                                         : WHICH<float, SPA_GATE_TOKEN>(__VA_ARGS__))       \
+                      : ((KIND) == SPA_GATE_NONE    ? WHICH<__nv_bfloat16, SPA_GATE_NONE>(__VA_ARGS__)  \
+                         : (KIND) == SPA_GATE_SCORE ? WHICH<__nv_bfloat16, SPA_GATE_SCORE>(__VA_ARGS__) \
+                         : (KIND) == SPA_GATE_IMAGE ? WHICH<__nv_bfloat16, SPA_GATE_IMAGE>(__VA_ARGS__) \
+                                                         : WHICH<__nv_bfloat16, SPA_GATE_TOKEN>(__VA_ARGS__)))
 
 }  // namespace
 
@@ -508,7 +754,7 @@ bool sandwich_supported(const spa_params& p) { return chunks_of(p) <= kMaxChunks
 
 size_t sandwich_workspace_bytes(const spa_params& p, const spa_sandwich& s) {
   const Plan pl = bwd_plan(p, s);
-  const size_t lines = (size_t)pl.ctas * kSums + (s.gate_kind == SPA_GATE_IMAGE ? (size_t)pl.units * 2 : 0);
+  const size_t lines = (size_t)pl.ctas * kSums + (pl.gate_kind == SPA_GATE_IMAGE ? ((size_t)pl.ctas + p.B) * 2 : 0);
   return lines * p.C * sizeof(float) + 256;
 }
 
@@ -519,20 +765,7 @@ int launch_sandwich(const spa_params& p, const spa_sandwich& s, const void* x, c
   a.out_y = (uint4*)y;
   a.out_n = (uint4*)n;
   a.stats = stats;
-#define SPA_FWD(T)                                                                                   \
-  do {                                                                                               \
-    const int w = warps_of(a.Q, 4), ch = (a.Q + 32 * w - 1) / (32 * w);                              \
-    if (w == 1 && ch == 1) return fwd_launch<T, 1, 1>(a, st);                                        \
-    if (w == 1 && ch == 2) return fwd_launch<T, 1, 2>(a, st);                                        \
-    if (w == 1 && ch == 3) return fwd_launch<T, 1, 3>(a, st);                                        \
-    if (w == 1) return fwd_launch<T, 1, 4>(a, st);                                                   \
-    if (w == 2) return ch <= 3 ? fwd_launch<T, 2, 3>(a, st) : fwd_launch<T, 2, 4>(a, st);            \
-    if (w == 4) return ch <= 3 ? fwd_launch<T, 4, 3>(a, st) : fwd_launch<T, 4, 4>(a, st);            \
-    return ch <= 3 ? fwd_launch<T, 8, 3>(a, st) : fwd_launch<T, 8, 4>(a, st);                        \
-  } while (0)
-  if (p.dtype == SPA_F32) SPA_FWD(float);
-  SPA_FWD(__nv_bfloat16);
-#undef SPA_FWD
+  return SPA_BY_GATE(s.gate_kind, fwd_by_warps, a, st);
 }
 
 int launch_sandwich_bwd(const spa_params& p, const spa_sandwich& s, const void* dn, const void* dy, const void* y, const void* z,
@@ -549,26 +782,15 @@ int launch_sandwich_bwd(const spa_params& p, const spa_sandwich& s, const void* 
   a.dgate = dgate;
   a.part = static_cast<float*>(workspace);
   a.part_gate = a.part + (size_t)pl.ctas * kSums * p.C;
-  a.units = pl.units;
-  a.splits = pl.splits;
-  int rc = SPA_OK;
-#define SPA_BWD(T)                                                                                   \
-  do {                                                                                               \
-    const bool one = a.Q <= 32 * pl.warps;                                                           \
-    if (pl.warps == 1) rc = one ? bwd_launch<T, 1, 1>(a, pl, st) : bwd_launch<T, 1, 2>(a, pl, st);   \
-    else if (pl.warps == 2) rc = bwd_launch<T, 2, 2>(a, pl, st);                                     \
-    else if (pl.warps == 4) rc = bwd_launch<T, 4, 2>(a, pl, st);                                     \
-    else if (pl.warps == 8) rc = bwd_launch<T, 8, 2>(a, pl, st);                                     \
-    else rc = bwd_launch<T, 16, 2>(a, pl, st);                                                       \
-  } while (0)
-  if (p.dtype == SPA_F32) SPA_BWD(float); else SPA_BWD(__nv_bfloat16);
-#undef SPA_BWD
+  a.rows_per_cta = pl.rows_per_cta;
+  a.gate_f32 = pl.gate_kind != s.gate_kind;
+  const int rc = SPA_BY_GATE(pl.gate_kind, bwd_by_warps, a, pl, st);
   if (rc != SPA_OK) return rc;
-  const bool images = s.gate_kind == SPA_GATE_IMAGE && dgate != nullptr;
+  const bool images = pl.gate_kind == SPA_GATE_IMAGE && dgate != nullptr;
   if (!images && dscale == nullptr && dg_post == nullptr && db_post == nullptr && dg_pre == nullptr && db_pre == nullptr) return SPA_OK;
   const dim3 grid(images ? 1 + p.B : 1, (p.C + 31) / 32);
 #define SPA_JOIN(T)                                                                                                       \
-  launch_pdl(sandwich_join_kernel<T>, grid, 32 * kJoinLanes, 0, st, a.part, a.part_gate, pl.ctas, pl.splits, p.C,         \
+  launch_pdl(sandwich_join_kernel<T>, grid, 32 * kJoinLanes, 0, st, a.part, a.part_gate, pl.ctas, p.N, pl.rows_per_cta, p.C, \
              (const T*)s.scale, (const T*)s.g_post, (const T*)s.b_post, (float*)dgate, dscale, dg_post, db_post, dg_pre, db_pre)
   if (p.dtype == SPA_F32) SPA_JOIN(float); else SPA_JOIN(__nv_bfloat16);
 #undef SPA_JOIN
