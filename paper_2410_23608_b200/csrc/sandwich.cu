@@ -47,6 +47,7 @@ struct Args {
   void* dgate;
   float *part, *part_gate;            // per CTA [kSums][C]; per unit of an image's rows [2][C]
   int rows, N, Q, C, z_rows, kind, rows_per_cta;
+  unsigned long long n_magic;         // t / N = t * n_magic >> 40 for t, N <= 2^20: n_magic = 2^40 / N + 1 is off by N / 2^40 at most
   bool gate_f32;                      // dgate of a gate per token: fp32
   float eps;
 };
@@ -54,32 +55,58 @@ struct Args {
 // The rows that a group has on their way, in shared memory: a thread copies its own chunks of the kA arrays of a row, asynchronously,
 // kDepth rows ahead (registers hold one row ahead at most: 16 rows of 1.5 KB per SM in flight instead of 64, 18 432 rows of 768
 // backward 47 us), and its warp's first lanes the row's scalars.  Nobody else reads them but the warp.
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 template <int kA, int kCh, int kDepth, int kThreads> struct Ring {
   static constexpr int kSlot = kA * kCh * kThreads * 16, kScalars = kThreads / 32 * 32;
   static constexpr int kBytes = kDepth * (kSlot + kScalars);
-  uint8_t* base;
-  int slot;
-  __device__ __forceinline__ uint8_t* chunk(int array, int k) const {
-    return base + slot * kSlot + ((array * kCh + k) * kThreads + (int)threadIdx.x) * 16;
+  uint32_t base, at, scalar;  // addresses in shared memory: the ring's, this thread's first chunk and its warp's scalars of the slot
+  __device__ __forceinline__ explicit Ring(uint32_t b) : base(b) { rewind(); }
+  __device__ __forceinline__ void rewind() {
+    at = base + threadIdx.x * 16;
+    scalar = base + kDepth * kSlot + (threadIdx.x >> 5) * 32;
   }
-  __device__ __forceinline__ float* scalars() const {  // eight of this warp
-    return reinterpret_cast<float*>(base + kDepth * kSlot + slot * kScalars) + (threadIdx.x >> 5) * 8;
+  __device__ __forceinline__ void next() {
+    at += kSlot;
+    scalar += kScalars;
+    if (at >= base + kDepth * kSlot) rewind();
   }
+  static constexpr int kArray = kCh * kThreads * 16, kChunk = kThreads * 16;
   __device__ __forceinline__ void copy(int array, int k, const uint4* from) const {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(chunk(array, k))), "l"(__cvta_generic_to_global(from)) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + array * kArray + k * kChunk), "l"(__cvta_generic_to_global(from)) : "memory");
   }
   __device__ __forceinline__ void copy_scalar(int i, const float* from) const {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(scalars() + i)), "l"(__cvta_generic_to_global(from)) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scalar + 4 * i), "l"(__cvta_generic_to_global(from)) : "memory");
   }
-  __device__ __forceinline__ uint4 get(int array, int k) const { return *reinterpret_cast<const uint4*>(chunk(array, k)); }
-  __device__ __forceinline__ void next() { slot = slot + 1 == kDepth ? 0 : slot + 1; }
+  __device__ __forceinline__ uint4 get(int array, int k) const { return lds16(at + array * kArray + k * kChunk); }
+  __device__ __forceinline__ float4 scalars() const {
+    const uint4 v = lds16(scalar);
+    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+  }
+  __device__ __forceinline__ float fifth() const { return ptx::lds_f32(scalar + 16); }
+  // Chunks past the end of a row are never copied: they are read as zeros, like the others, when they have been cleared once.
+  __device__ __forceinline__ void clear(int t0, int stride, int Q) {
+    for (int slot = 0; slot < kDepth; ++slot, next())
+#pragma unroll
+      for (int k = 0; k < kCh; ++k)
+        if (t0 + stride * k >= Q) {
+#pragma unroll
+          for (int i = 0; i < kA; ++i) sts16(at + i * kArray + k * kChunk, make_uint4(0u, 0u, 0u, 0u));
+        }
+  }
 };
 
-// Sums of kN values over the group's threads, in every one of them.  Calls alternate between two lines of `red`: a warp that
+// Sums of kN values over the group's threads, in every one of them.  Calls alternate between two lines: a warp that
 // writes a line again has met the others at the barrier in between, behind their reads of it.
 template <int W> struct GroupSum {
-  float* red;  // [2][W][4] of this group
-  int id, warp, lane, turn;
+  uint32_t line, other;  // [W][4] floats of this group each, in shared memory
+  int id, warp, lane;
   template <int kN> __device__ __forceinline__ void operator()(float (&v)[kN]) {
     static_assert(kN <= 3, "a line has room for four");
     // two values at once: half of the lanes carries each of them through the last four steps
@@ -101,21 +128,21 @@ template <int W> struct GroupSum {
       for (int o = 16; o > 0; o >>= 1) v[kN - 1] += __shfl_xor_sync(0xffffffffu, v[kN - 1], o);
     }
     if constexpr (W > 1) {
-      float* line = red + turn * 4 * W;
-      if (lane == 0) line[4 * warp] = v[0];
-      if (kN >= 2 && lane == 16) line[4 * warp + 1] = v[1];
-      if (kN == 3 && lane == 0) line[4 * warp + 2] = v[2];
+      const uint32_t mine = line + 16 * warp;
+      if (lane == 0) ptx::sts_s32(mine, __float_as_int(v[0]));
+      if (kN >= 2 && lane == 16) ptx::sts_s32(mine + 4, __float_as_int(v[1]));
+      if (kN == 3 && lane == 0) ptx::sts_s32(mine + 8, __float_as_int(v[2]));
       asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "n"(32 * W) : "memory");
 #pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] = 0.f;
-#pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float4 l = *reinterpret_cast<const float4*>(line + 4 * w);
-        v[0] += l.x;
-        if (kN >= 2) v[1] += l.y;
-        if (kN == 3) v[2] += l.z;
+        const uint4 l = lds16(line + 16 * w);
+        v[0] = w == 0 ? __uint_as_float(l.x) : v[0] + __uint_as_float(l.x);
+        if (kN >= 2) v[1] = w == 0 ? __uint_as_float(l.y) : v[1] + __uint_as_float(l.y);
+        if (kN == 3) v[2] = w == 0 ? __uint_as_float(l.z) : v[2] + __uint_as_float(l.z);
       }
-      turn ^= 1;
+      const uint32_t t = line;
+      line = other;
+      other = t;
     }
   }
 };
@@ -172,12 +199,13 @@ template <int kGate> constexpr int kFwdArrays = kGateRows<kGate> ? 3 : 2;
 constexpr int kFwdDepth = 4;
 
 template <typename T, int W, int kCh, int kGate>
-__global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(const Args a) {
+__global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / threads_of(W, false) : 1) sandwich_fwd_kernel(const Args a) {
   pdl_entry();
   constexpr int P = kPairs<T>, G = 32 * W;
   __shared__ __align__(16) float red[groups_of(W, false) * 8 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  GroupSum<W> sum{red + grp * 8 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
+  const uint32_t lines = ptx::smem_u32(red + grp * 8 * W);
+  GroupSum<W> sum{lines, lines + 16 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
   const float inv_c = 1.f / a.C;
   const bool layer = a.kind == SPA_NORM_LAYER;
   // y = x + gate (cw zh + cb), n = cp norm(y) + bp
@@ -221,21 +249,21 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
     rstd = rsqrtf(t[0] * inv_c + a.eps);
   };
   extern __shared__ __align__(16) uint8_t ring_s[];
-  Ring<kFwdArrays<kGate>, kCh, kFwdDepth, threads_of(W, false)> ring{ring_s, 0};
+  Ring<kFwdArrays<kGate>, kCh, kFwdDepth, threads_of(W, false)> ring(ptx::smem_u32(ring_s));
   auto row_of = [&](int t) { return a.z_row != nullptr && t < a.rows ? ld_dep(a.z_row + t) : t; };
   auto has_row = [&](int zr) { return zr >= 0 && zr < a.z_rows; };
   auto fetch = [&](int t, int zr) {
     if (t < a.rows) {
-      const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
-      const uint4* gate16 = static_cast<const uint4*>(a.gate) + (kGate == SPA_GATE_IMAGE ? (long long)(t / a.N) * a.Q : at);
+      // places in chunks: below 2^30
+      const unsigned at = t * a.Q + t0, zat = zr * a.Q + t0;
+      const unsigned gat = kGate == SPA_GATE_IMAGE ? (unsigned)((unsigned long long)t * a.n_magic >> 40) * a.Q + t0 : at;
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
-        const int q = t0 + G * k;
-        if (q < a.Q) {
-          ring.copy(0, k, a.x + at + q);
+        if (t0 + G * k < a.Q) {
+          ring.copy(0, k, a.x + (at + G * k));
           if (has_row(zr)) {
-            ring.copy(1, k, a.z + zat + q);
-            if (kGateRows<kGate>) ring.copy(kGateRows<kGate> ? 2 : 0, k, gate16 + q);
+            ring.copy(1, k, a.z + (zat + G * k));
+            if (kGateRows<kGate>) ring.copy(kGateRows<kGate> ? 2 : 0, k, static_cast<const uint4*>(a.gate) + (gat + G * k));
           }
         }
       }
@@ -245,6 +273,7 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
   };
   const int step = gridDim.x * groups_of(W, false);
   int t = blockIdx.x * groups_of(W, false) + grp;
+  ring.clear(t0, G, a.Q);
   int zr[kFwdDepth + 1];  // rows of z of the tokens on their way, and of one more
 #pragma unroll
   for (int i = 0; i <= kFwdDepth; ++i) zr[i] = row_of(t + i * step);
@@ -258,15 +287,13 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
     cp_async_wait<kFwdDepth - 1>();
     __syncwarp();
     uint4 xr[kCh], zv[kCh], gr[kCh];
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
     for (int k = 0; k < kCh; ++k) {
-      const bool in = t0 + G * k < a.Q;
-      xr[k] = in ? ring.get(0, k) : zero;
-      zv[k] = in && has ? ring.get(1, k) : zero;
-      gr[k] = in && has && kGateRows<kGate> ? ring.get(kGateRows<kGate> ? 2 : 0, k) : zero;
+      xr[k] = ring.get(0, k);
+      zv[k] = ring.get(1, k);  // without a row: what was there, and is not used
+      if (kGateRows<kGate>) gr[k] = ring.get(kGateRows<kGate> ? 2 : 0, k);
     }
-    const float score = kGate == SPA_GATE_SCORE ? ring.scalars()[0] : 0.f;
+    const float score = kGate == SPA_GATE_SCORE ? ring.scalars().x : 0.f;
     __syncwarp();
     fetch(t + kFwdDepth * step, zr[kFwdDepth]);
     ring.next();
@@ -275,7 +302,7 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
     zr[kFwdDepth] = row_of(t + (kFwdDepth + 1) * step);
     uint64_t v[kCh][P];
     float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
-    const long long at = (long long)t * a.Q;
+    const unsigned at = t * a.Q + t0;
     if (has) {
 #pragma unroll
       for (int k = 0; k < kCh; ++k) to_pairs(zv[k], v[k]);
@@ -291,7 +318,7 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
           const uint64_t b = fma2(fma2(v[k][i], r, m), cw[k][i], cb[k][i]);
           v[k][i] = kGate == SPA_GATE_NONE ? add2(b, x[i]) : fma2(b, kGateRows<kGate> ? g[i] : w, x[i]);
         }
-        if (t0 + G * k < a.Q) a.out_y[at + t0 + G * k] = from_pairs(v[k]);
+        if (t0 + G * k < a.Q) a.out_y[at + G * k] = from_pairs(v[k]);
         else {
 #pragma unroll
           for (int i = 0; i < P; ++i) v[k][i] = 0ull;
@@ -301,7 +328,7 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
         to_pairs(xr[k], v[k]);
-        if (t0 + G * k < a.Q) a.out_y[at + t0 + G * k] = xr[k];
+        if (t0 + G * k < a.Q) a.out_y[at + G * k] = xr[k];
       }
     }
     if (a.out_n != nullptr) {
@@ -312,7 +339,7 @@ __global__ void __launch_bounds__(threads_of(W, false)) sandwich_fwd_kernel(cons
         if (t0 + G * k < a.Q) {
 #pragma unroll
           for (int i = 0; i < P; ++i) v[k][i] = fma2(fma2(v[k][i], r, m), cp[k][i], bp[k][i]);
-          a.out_n[at + t0 + G * k] = from_pairs(v[k]);
+          a.out_n[at + G * k] = from_pairs(v[k]);
         }
       }
     }
@@ -343,7 +370,8 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
   float* acc_s = reinterpret_cast<float*>(smem);
   __shared__ __align__(16) float red[kG * 8 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  GroupSum<W> sum{red + grp * 8 * W, grp, t0 >> 5, (int)threadIdx.x & 31, 0};
+  const uint32_t lines = ptx::smem_u32(red + grp * 8 * W);
+  GroupSum<W> sum{lines, lines + 16 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
   const float inv_c = 1.f / a.C;
   const bool layer = a.kind == SPA_NORM_LAYER;
   uint64_t sA[kCh][P] = {}, sB[kCh][P] = {}, sG[kCh][P] = {}, sN[kCh][P] = {};
@@ -376,59 +404,59 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
   };
   // gz = d gate cw; a / gate = cw zh + cb (for the gradient of a gate that is not per image)
   uint64_t cp[kCh][P], cw[kCh][P], cb[kCh][P];
+  auto products = [&](const uint4* gate) {  // with a gate per image, cw holds the image's gate too
 #pragma unroll
-  for (int k = 0; k < kCh; ++k) {
-    const int q = t0 + G * k;
-    const bool in = q < a.Q;
-    uint64_t sc[P];
-    param<T>(a.scale, q, in, 1.f, sc);
-    param<T>(a.g_post, q, in, 1.f, cw[k]);
-    param<T>(a.g_pre, q, in, 1.f, cp[k]);
-    param<T>(a.b_post, q, in, 0.f, cb[k]);
+    for (int k = 0; k < kCh; ++k) {
+      const int q = t0 + G * k;
+      const bool in = q < a.Q;
+      uint64_t sc[P], g[P];
+      param<T>(a.scale, q, in, 1.f, sc);
+      param<T>(a.g_post, q, in, 1.f, cw[k]);
+      param<T>(a.b_post, q, in, 0.f, cb[k]);
+      if (kImage) param<T>(gate, q, in, 0.f, g);
 #pragma unroll
-    for (int i = 0; i < P; ++i) { cw[k][i] = mul2(cw[k][i], sc[i]); cb[k][i] = mul2(cb[k][i], sc[i]); }
-  }
+      for (int i = 0; i < P; ++i) {
+        cw[k][i] = mul2(cw[k][i], kImage ? mul2(sc[i], g[i]) : sc[i]);
+        cb[k][i] = mul2(cb[k][i], sc[i]);
+      }
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kCh; ++k) param<T>(a.g_pre, t0 + G * k, t0 + G * k < a.Q, 1.f, cp[k]);
+  if (!kImage) products(nullptr);
   struct Row { uint4 n[kCh], y[kCh], d[kCh], z[kCh], g[kGate == SPA_GATE_TOKEN ? kCh : 1]; float m1, r1, m2, r2, score; int zr; };
-  Rows ring{smem, 0};
+  Rows ring(ptx::smem_u32(smem));
   auto has_row = [&](int zr) { return zr >= 0 && zr < a.z_rows; };
   const int share = blockIdx.x * a.rows_per_cta, share_end = share + a.rows_per_cta < a.rows ? share + a.rows_per_cta : a.rows;
   for (int begin = share, end; begin < share_end; begin = end) {
     const int image = kImage ? begin / a.N : 0;
     end = kImage && (image + 1) * a.N < share_end ? (image + 1) * a.N : share_end;
-    uint64_t cg[kCh][P];  // gate per image: cw times it
-    if (kImage) {
-#pragma unroll
-      for (int k = 0; k < kCh; ++k) {
-        param<T>(static_cast<const uint4*>(a.gate) + (long long)image * a.Q, t0 + G * k, t0 + G * k < a.Q, 0.f, cg[k]);
-#pragma unroll
-        for (int i = 0; i < P; ++i) cg[k][i] = mul2(cg[k][i], cw[k][i]);
-      }
-    }
+    if (kImage) products(static_cast<const uint4*>(a.gate) + (long long)image * a.Q);
     auto row_of = [&](int t) { return a.z_row != nullptr && t < end ? ld_dep(a.z_row + t) : t; };
     auto fetch = [&](int t, int zr) {
       if (t < end) {
         const bool has = has_row(zr);
-        const long long at = (long long)t * a.Q, zat = (long long)zr * a.Q;
+        const unsigned at = t * a.Q + t0, zat = zr * a.Q + t0;  // places in chunks: below 2^30
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
-          const int q = t0 + G * k;
-          if (q < a.Q) {
+          if (t0 + G * k < a.Q) {
             if (a.dn != nullptr) {
-              ring.copy(0, k, a.dn + at + q);
-              ring.copy(1, k, a.y + at + q);
+              ring.copy(0, k, a.dn + (at + G * k));
+              ring.copy(1, k, a.y + (at + G * k));
             }
-            if (a.dy != nullptr) ring.copy(2, k, a.dy + at + q);
+            if (a.dy != nullptr) ring.copy(2, k, a.dy + (at + G * k));
             if (has) {
-              ring.copy(3, k, a.z + zat + q);
-              if (kGate == SPA_GATE_TOKEN) ring.copy(kGate == SPA_GATE_TOKEN ? 4 : 0, k, static_cast<const uint4*>(a.gate) + at + q);
+              ring.copy(3, k, a.z + (zat + G * k));
+              if (kGate == SPA_GATE_TOKEN) ring.copy(kGate == SPA_GATE_TOKEN ? 4 : 0, k, static_cast<const uint4*>(a.gate) + (at + G * k));
             }
           }
         }
-        if (sum.lane < 4) ring.copy_scalar(sum.lane, a.stats + (long long)sum.lane * a.rows + t);
+        if (sum.lane < 4) ring.copy_scalar(sum.lane, a.stats + (unsigned)(sum.lane * a.rows + t));
         if (kGate == SPA_GATE_SCORE && sum.lane == 4) ring.copy_scalar(4, static_cast<const float*>(a.gate) + t);
       }
       cp_async_commit();
     };
+    ring.clear(t0, G, a.Q);
     int t = begin + grp, zr[kDepth + 1];  // rows of z of the tokens on their way, and of one more
 #pragma unroll
     for (int i = 0; i <= kDepth; ++i) zr[i] = row_of(t + i * kG);
@@ -442,24 +470,21 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
       __syncwarp();
       Row cur;
       {
-        const bool has = has_row(zr[0]);
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-        cur.zr = has ? zr[0] : -1;
+        cur.zr = has_row(zr[0]) ? zr[0] : -1;
 #pragma unroll
-        for (int k = 0; k < kCh; ++k) {
-          const bool in = t0 + G * k < a.Q;
-          cur.n[k] = in && a.dn != nullptr ? ring.get(0, k) : zero;
-          cur.y[k] = in && a.dn != nullptr ? ring.get(1, k) : zero;
-          cur.d[k] = in && a.dy != nullptr ? ring.get(2, k) : zero;
-          cur.z[k] = in && has ? ring.get(3, k) : zero;
-          if constexpr (kGate == SPA_GATE_TOKEN) cur.g[k] = in && has ? ring.get(4, k) : zero;
+        for (int k = 0; k < kCh; ++k) {  // of absent arrays and rows: what was there, and is not used
+          cur.n[k] = ring.get(0, k);
+          cur.y[k] = ring.get(1, k);
+          cur.d[k] = a.dy != nullptr ? ring.get(2, k) : make_uint4(0u, 0u, 0u, 0u);
+          cur.z[k] = ring.get(3, k);
+          if constexpr (kGate == SPA_GATE_TOKEN) cur.g[k] = ring.get(4, k);
         }
-        const float* sc = ring.scalars();
-        cur.m1 = sc[0];
-        cur.r1 = sc[1];
-        cur.m2 = sc[2];
-        cur.r2 = sc[3];
-        cur.score = kGate == SPA_GATE_SCORE ? sc[4] : 0.f;
+        const float4 sc = ring.scalars();
+        cur.m1 = sc.x;
+        cur.r1 = sc.y;
+        cur.m2 = sc.z;
+        cur.r2 = sc.w;
+        cur.score = kGate == SPA_GATE_SCORE ? ring.fifth() : 0.f;
       }
       __syncwarp();
       fetch(t + kDepth * kG, zr[kDepth]);
@@ -467,7 +492,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 #pragma unroll
       for (int i = 0; i < kDepth; ++i) zr[i] = zr[i + 1];
       zr[kDepth] = row_of(t + (kDepth + 1) * kG);
-      const long long at = (long long)t * a.Q, zat = (long long)cur.zr * a.Q;
+      const unsigned at = t * a.Q + t0, zat = cur.zr * a.Q + t0;
       const bool has = cur.zr >= 0;
       // ---- through the norm behind the sum: d, the gradient of y
       uint64_t d[kCh][P];
@@ -506,7 +531,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
       }
 #pragma unroll
       for (int k = 0; k < kCh; ++k)
-        if (t0 + G * k < a.Q) a.dx[at + t0 + G * k] = from_pairs(d[k]);
+        if (t0 + G * k < a.Q) a.dx[at + G * k] = from_pairs(d[k]);
       if (has) {
         const float score = kGate == SPA_GATE_SCORE ? sigmoid(cur.score) : 1.f;
         const uint64_t r = both(cur.r1), m = both(-cur.m1 * cur.r1), w = both(score);
@@ -519,7 +544,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
           if constexpr (kGate == SPA_GATE_TOKEN) to_pairs(cur.g[k], g);
 #pragma unroll
           for (int i = 0; i < P; ++i) {
-            if (!in) d[k][i] = 0ull;
+            if (!in) d[k][i] = 0ull;  // the means' part
             zh[k][i] = fma2(zh[k][i], r, m);
             if (kGate == SPA_GATE_SCORE) u3 = fma2(d[k][i], fma2(zh[k][i], cw[k][i], cb[k][i]), u3);
             if constexpr (kGate == SPA_GATE_TOKEN) {
@@ -530,7 +555,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
             if (kGate == SPA_GATE_SCORE) d[k][i] = mul2(d[k][i], w);
             sA[k][i] = fma2(d[k][i], zh[k][i], sA[k][i]);
             sB[k][i] = add2(sB[k][i], d[k][i]);
-            d[k][i] = mul2(d[k][i], kImage ? cg[k][i] : cw[k][i]);  // gz
+            d[k][i] = mul2(d[k][i], cw[k][i]);  // gz
             u1 = add2(u1, d[k][i]);
             u2 = fma2(d[k][i], zh[k][i], u2);
           }
@@ -539,9 +564,9 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
               if (a.gate_f32) {
 #pragma unroll
                 for (int i = 0; i < P; i += 2)
-                  static_cast<ulonglong2*>(a.dgate)[((at + t0 + G * k) * P + i) / 2] = make_ulonglong2(g[i], g[i + 1]);
+                  static_cast<ulonglong2*>(a.dgate)[(size_t)(at + G * k) * (P / 2) + i / 2] = make_ulonglong2(g[i], g[i + 1]);
               } else {
-                static_cast<uint4*>(a.dgate)[at + t0 + G * k] = from_pairs(g);
+                static_cast<uint4*>(a.dgate)[at + G * k] = from_pairs(g);
               }
             }
           }
@@ -560,7 +585,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
           if (t0 + G * k < a.Q) {
 #pragma unroll
             for (int i = 0; i < P; ++i) d[k][i] = fma2(d[k][i], r, fma2(zh[k][i], a2, a1));
-            a.dz[zat + t0 + G * k] = from_pairs(d[k]);
+            a.dz[zat + G * k] = from_pairs(d[k]);
           }
         }
       } else if (a.dgate != nullptr) {
@@ -571,7 +596,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
             if (t0 + G * k < a.Q) {
 #pragma unroll
               for (int i = 0; i < (a.gate_f32 ? P / 2 : 1); ++i)
-                static_cast<uint4*>(a.dgate)[(at + t0 + G * k) * (a.gate_f32 ? P / 2 : 1) + i] = make_uint4(0u, 0u, 0u, 0u);
+                static_cast<uint4*>(a.dgate)[(size_t)(at + G * k) * (a.gate_f32 ? P / 2 : 1) + i] = make_uint4(0u, 0u, 0u, 0u);
             }
         }
       }
@@ -685,6 +710,7 @@ Args args_of(const spa_params& p, const spa_sandwich& s, const void* z, const in
   a.b_pre = (const uint4*)s.b_pre;
   a.rows = p.B * p.N;
   a.N = p.N;
+  a.n_magic = (1ull << 40) / p.N + 1;
   a.Q = chunks_of(p);
   a.C = p.C;
   a.z_rows = z_row != nullptr ? p.capacity : p.B * p.N;
