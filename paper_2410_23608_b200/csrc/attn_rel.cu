@@ -2,6 +2,8 @@
 // expanded to one value per offset, the tokens' positions, the bounds that the table's gradient is scaled by) and behind them
 // (the gradient from its integer bins).  The backbone that the paper's blocks belong to (Sec. 3.1) has such a bias in every
 // attention; with packed rows it goes by the tokens' places on the grid, which idx keeps.
+#include <math_constants.h>
+
 #include "attn_rel.cuh"
 #include "spa_tc.cuh"
 
@@ -19,6 +21,7 @@ struct Prep {
   const void *qkv, *dao;  // backward only
   float* bias;
   int32_t *pos, *owner, *bad;
+  uint32_t* redo;
   unsigned long long* acc;
   float* bound;
   int n_seg, capacity, B, N, rows, cols, n_buckets, entries, pitch, C, H;
@@ -64,6 +67,7 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   if constexpr (kBwd) {
     for (int i = tid; i < a.n_buckets * a.H; i += all) a.acc[i] = 0ull;
     for (int i = tid; i < a.H; i += all) a.bad[i] = 0;
+    if (tid == 0) *a.redo = 0u;
     __syncthreads();
     // A thread has one chunk of a row, the same one of every row it looks at, and neighbouring lanes the other chunks of its head:
     // whole lines per load, and a maximum per thread.  (A thread per row and head read its line in eight loads, which went to L2
@@ -113,9 +117,59 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   }
 }
 
-// dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.
-__global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const int32_t* seg, int n_seg, int capacity, const int32_t* idx,
-                                                         const int32_t* owner, int tokens, float* __restrict__ dtable, int32_t* d_status) {
+// A half of a row of dQ, or of dK and dV, from the rows of its own segment (see rel_redo), by a warp: the pairs to its lanes.
+struct Redo {
+  RelView view;
+  const __nv_bfloat16 *qkv, *dao;
+  const float *lse, *delta;
+  __nv_bfloat16* dqkv;
+  int C, d;
+  float scale;
+};
+__device__ void redo_row(const Redo& r, const int32_t* seg, int n_seg, int capacity, int Np, uint32_t what) {
+  const int row = what & 0xfffff, h = (what >> 20) & 0xff, half = (what >> 29) & 1, lane = threadIdx.x & 31, n = r.d / 2;
+  const bool keys = (what >> 28) & 1;
+  const long long ld = 3LL * r.C;
+  const int col = h * r.d;
+  const RowSeg s = row_segment(seg, n_seg, Np, row);
+  const float* bias = r.view.bias + (long long)h * r.view.pitch + r.view.center;
+  for (int e0 = half * n; e0 < half * n + n; e0 += 8) {
+    float acc1[8] = {}, acc2[8] = {};
+    for (int k = s.lo + lane; k < s.hi; k += 32) {
+      const int q = keys ? k : row, j = keys ? row : k;
+      const __nv_bfloat16 *Q = r.qkv + q * ld + col, *K = r.qkv + j * ld + r.C + col, *dO = r.dao + (long long)q * r.C + col;
+      float dot = 0.f, dp = 0.f;
+      for (int e = 0; e < r.d; ++e) {
+        dot = fmaf(__bfloat162float(Q[e]), __bfloat162float(K[e]), dot);
+        dp = fmaf(__bfloat162float(dO[e]), __bfloat162float(K[r.C + e]), dp);
+      }
+      const float l = r.lse[(long long)h * capacity + q];
+      const float p = l == -CUDART_INF_F ? 0.f : exp2f(fmaf(dot, r.scale * kLog2e, bias[r.view.pos[q] - r.view.pos[j]]) - l * kLog2e);
+      const float ds = p * (dp - r.delta[(long long)h * capacity + q]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        acc1[e] = fmaf(ds, __bfloat162float((keys ? Q : K)[e0 + e]), acc1[e]);
+        acc2[e] = fmaf(p, __bfloat162float(dO[e0 + e]), acc2[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      acc1[e] = warp_sum(acc1[e]) * r.scale;
+      acc2[e] = warp_sum(acc2[e]);
+    }
+    if (lane == 0) {
+      *reinterpret_cast<uint4*>(r.dqkv + row * ld + (keys ? r.C : 0) + col + e0) = Vec16<__nv_bfloat16>::from_float(acc1);
+      if (keys) *reinterpret_cast<uint4*>(r.dqkv + row * ld + 2 * r.C + col + e0) = Vec16<__nv_bfloat16>::from_float(acc2);
+    }
+  }
+}
+
+// dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.  kRedo: behind
+// the tensor-core kernels, the rows that they noted down.
+template <bool kRedo>
+__global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const Redo r, const int32_t* seg, int n_seg, int capacity,
+                                                         const int32_t* idx, const int32_t* owner, int tokens,
+                                                         float* __restrict__ dtable, int32_t* d_status) {
   pdl_entry();
   extern __shared__ float unit[];  // [H] value of a bin's least bit
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -126,18 +180,25 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
   }
   __syncthreads();
   const int tid = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
-  for (int i = tid; i < g.n_buckets * g.H; i += all) dtable[i] = (float)((double)(long long)g.acc[i] * (double)unit[i % g.H]);
+  for (int i = tid; i < g.n_buckets * g.H; i += all) {
+    const int h = i % g.H;
+    dtable[i] = (float)((double)(long long)g.acc[(long long)h * g.n_buckets + i / g.H] * (double)unit[h]);
+  }
   const int Np = packed_rows(seg, n_seg, capacity);
   for (int i = tid; i < Np; i += all) {
     const int t = ld_dep(idx + i);
     if ((unsigned)t < (unsigned)tokens && ld_dep(owner + t) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
+  }
+  if constexpr (kRedo) {
+    const int n = ld_dep(reinterpret_cast<const int32_t*>(g.redo));
+    for (int i = blockIdx.x * 8 + warp; i < n; i += gridDim.x * 8) redo_row(r, seg, n_seg, capacity, Np, g.redo[1 + i]);
   }
 }
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Layout {
-  size_t pos, bias, acc, bound, bad, owner, delta, end;
+  size_t pos, bias, acc, bound, bad, owner, delta, redo, end;
   int entries, pitch, center;
 };
 Layout layout(const spa_params& p, const spa_rel_bias& r) {
@@ -154,7 +215,12 @@ Layout layout(const spa_params& p, const spa_rel_bias& r) {
   l.bound = take((size_t)kRelBlocks * p.H * 8);
   l.bad = take((size_t)p.H * 4);
   l.owner = take((size_t)p.B * p.N * 4);
-  l.delta = take((size_t)p.H * p.capacity * 4);
+  if (use_tc(p)) {
+    l.delta = take((size_t)p.H * p.capacity * 4);
+    l.redo = take(((size_t)4 * p.H * p.capacity + 1) * 4);
+  } else {
+    l.delta = l.redo = take(4);
+  }
   l.end = at;
   return l;
 }
@@ -172,6 +238,7 @@ int launch_prep(const spa_params& p, const spa_rel_bias& r, const Layout& l, cha
   a.pos = (int32_t*)(ws + l.pos);
   a.owner = (int32_t*)(ws + l.owner);
   a.bad = (int32_t*)(ws + l.bad);
+  a.redo = (uint32_t*)(ws + l.redo);
   a.acc = (unsigned long long*)(ws + l.acc);
   a.bound = (float*)(ws + l.bound);
   a.n_seg = n_seg;
@@ -234,6 +301,7 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   g.bound = (const float*)(ws + l.bound);
   g.peak = peak;
   g.bad = (int32_t*)(ws + l.bad);
+  g.redo = (uint32_t*)(ws + l.redo);
   g.n_buckets = r.n_buckets;
   g.H = p.H;
   rc = tc ? launch_attention_rel_bwd_tc(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, (float*)(ws + l.delta), d_status, st)
@@ -241,8 +309,10 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   if (rc != SPA_OK) return rc;
   const long long work = (long long)r.n_buckets * p.H > p.capacity ? (long long)r.n_buckets * p.H : p.capacity;
   const int grid = (int)((work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
-  launch_pdl(rel_finish_kernel, grid, 256, (size_t)p.H * sizeof(float), st, g, seg, n_seg, p.capacity, idx,
-             (const int32_t*)(ws + l.owner), p.B * p.N, dtable, d_status);
+  const Redo redo{view(l, ws), (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, lse, (const float*)(ws + l.delta), (__nv_bfloat16*)dqkv,
+               p.C, p.C / p.H, softmax_scale_of(p)};
+  launch_pdl(tc ? rel_finish_kernel<true> : rel_finish_kernel<false>, grid, 256, (size_t)p.H * sizeof(float), st, g, redo, seg, n_seg, p.capacity,
+             idx, (const int32_t*)(ws + l.owner), p.B * p.N, dtable, d_status);
   SPA_CUDA_CHECK_LAUNCH("rel_finish_kernel");
   return SPA_OK;
 }

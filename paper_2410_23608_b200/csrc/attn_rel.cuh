@@ -22,13 +22,20 @@ struct RelView {          // what the forward and backward kernels read
 
 constexpr int kRelBlocks = kNumSMs;  // CTAs of the kernel that prepares a call, each with its own maxima
 struct RelGrad {
-  unsigned long long* acc;  // [n_buckets][H] sums of dS times 2^(kRelBits - exponent of the head's bound)
+  unsigned long long* acc;  // [H][n_buckets] sums of dS times 2^(kRelBits - exponent of the head's bound)
   const int32_t* bucket;    // [entries]
   const float* bound;       // [kRelBlocks][H][2] largest |v_j|^2 and |dO_i|^2
   const float* peak;        // [H][capacity] log of the row's largest probability, optional
   int32_t* bad;             // [H] a row's statistics are not finite
+  uint32_t* redo;           // [1 + 4 H capacity] how many, and which parts of rows are to be formed again
   int n_buckets, H;
 };
+
+// A zero weight times an infinity or NaN of another segment in the same tile is NaN.  Halves of rows of dQ (keys = false) or of dK
+// and dV that are not finite are noted down, and formed again behind the attention from their own segment's rows alone.
+__device__ __forceinline__ void rel_redo(const RelGrad& g, bool keys, int half, int h, int row) {
+  g.redo[1 + atomicAdd(g.redo, 1u)] = (uint32_t)row | (uint32_t)h << 20 | (keys ? 1u : 0u) << 28 | (uint32_t)half << 29;
+}
 
 // Bits of the head's bound.  A bin has at most one pair per query, 2^20 in all, and the bound is taken up to a power of two.
 constexpr int kRelBits = 40;
@@ -70,7 +77,7 @@ __device__ __forceinline__ void rel_check_row(const RelGrad& g, int h, float lse
 // v to the bin of the bucket of table entry `at`
 __device__ __forceinline__ void rel_add(const RelGrad& g, int h, int at, long long v) {
   const int b = g.bucket[at];
-  if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)b * g.H + h, (unsigned long long)v);
+  if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)h * g.n_buckets + b, (unsigned long long)v);
 }
 
 int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,

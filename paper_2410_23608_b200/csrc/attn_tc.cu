@@ -696,47 +696,11 @@ template <int D, bool kDQ, int kRel = kNoRel> __host__ __device__ constexpr int 
 struct RelBwd {
   RelView view;
   RelGrad grad;
-  const __nv_bfloat16 *qkv, *dao;
   bool shared_bins;
 };
 // The scale of an item's bins.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
 // with |dS| below 2^kRelItemBits in units of the scale a sum stays below 2^30.
 constexpr int kRelItemBits = 23;
-
-// kN head dimensions from column `col` + `first` on of a row's gradient (dQ; dK and dV) from the rows of its segment alone: rare, one
-// pair after the other from global memory.
-template <int kN>
-__device__ __noinline__ void rel_grad_again(bool dq, const RelBwd& r, const float* lse, const float* delta, __nv_bfloat16* dqkv, int C,
-                                            int capacity, int h, int d, int first, int row, int lo, int hi, float scale) {
-  const long long ld = 3LL * C;
-  const int col = h * d;
-  const float* bias = r.view.bias + (long long)h * r.view.pitch + r.view.center;
-  for (int e0 = first; e0 < first + kN; e0 += 8) {
-    float acc1[8] = {}, acc2[8] = {};
-    for (int k = lo; k < hi; ++k) {
-      const int q = dq ? row : k, j = dq ? k : row;
-      const __nv_bfloat16 *Q = r.qkv + q * ld + col, *K = r.qkv + j * ld + C + col, *dO = r.dao + (long long)q * C + col;
-      float s = 0.f, dp = 0.f;
-      for (int e = 0; e < d; ++e) {
-        s = fmaf(__bfloat162float(Q[e]), __bfloat162float(K[e]), s);
-        dp = fmaf(__bfloat162float(dO[e]), __bfloat162float(K[C + e]), dp);
-      }
-      const float l = lse[(long long)h * capacity + q];
-      const float b = bias[r.view.pos[q] - r.view.pos[j]];
-      const float p = l == -CUDART_INF_F ? 0.f : ptx::ex2_approx(fmaf(s, scale * 1.4426950408889634f, b) - l * 1.4426950408889634f);
-      const float ds = p * (dp - delta[(long long)h * capacity + q]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        acc1[e] = fmaf(ds, __bfloat162float((dq ? K : Q)[e0 + e]), acc1[e]);
-        acc2[e] = fmaf(p, __bfloat162float(dO[e0 + e]), acc2[e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc1[e] *= scale;
-    *reinterpret_cast<uint4*>(dqkv + row * ld + (dq ? 0 : C) + col + e0) = Vec16<__nv_bfloat16>::from_float(acc1);
-    if (!dq) *reinterpret_cast<uint4*>(dqkv + row * ld + 2 * C + col + e0) = Vec16<__nv_bfloat16>::from_float(acc2);
-  }
-}
 
 template <int D, bool kDQ, bool kLoop, int kRel>
 __global__ void __launch_bounds__(kBwdThreads, 2)
@@ -1310,11 +1274,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
           if (v != 0) rel_add(rel.grad, h, i, shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63));
         }
       }
-      // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, from their own segment
-      if (__syncthreads_or(again)) {
-        if (again && mine.hi > mine.lo)
-          rel_grad_again<kDh>(kDQ, rel, lse, delta, dqkv, C, capacity, h, D, half * kDh, row, mine.lo, mine.hi, scale);
-      }
+      if (again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
     }
   }
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
@@ -1811,12 +1771,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     __syncthreads();
     copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
     copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
-    if constexpr (kRel != kNoRel) {  // see the dQ pass
-      if (__syncthreads_or(again)) {
-        if (again && mine.hi > mine.lo)
-          rel_grad_again<kDh>(false, rel, lse, delta, dqkv, C, capacity, h, D, half * kDh, row, mine.lo, mine.hi, scale);
-      }
-    }
+    if (kRel != kNoRel && again && mine.hi > mine.lo) rel_redo(rel.grad, true, half, h, row);
   }
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
     for (int t = issued > kStages ? issued - kStages : 0; t < issued; ++t) ptx::mbar_wait(bar_y(stage_of(t)), use_of(t));
@@ -2202,7 +2157,7 @@ int launch_attention_bwd_tc(const spa_params& p, const void* qkv, const void* ao
 int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                                 const int32_t* seg, int n_seg, const RelView& view, const RelGrad& grad, void* dqkv, float* delta,
                                 int32_t* d_status, cudaStream_t st) {
-  const RelBwd rel{view, grad, (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, true};
+  const RelBwd rel{view, grad, true};
   const int table = view.pitch * 4;
   if (p.C / p.H == 64) {
     if (bwd_smem_bytes<64, true, kRelShared>() + 2 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
