@@ -80,6 +80,28 @@ __device__ __forceinline__ void rel_add(const RelGrad& g, int h, int at, long lo
   if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)h * g.n_buckets + b, (unsigned long long)v);
 }
 
+// What the kernels with a bias by relative position are given beside the others' arguments.  shared_bins: the table's gradient is
+// summed in shared memory, item by item; else pair by pair in global memory.
+struct RelBwd {
+  RelView view;
+  RelGrad grad;
+  bool shared_bins;
+};
+// The scale of an item's bins.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
+// with |dS| below 2^kRelItemBits in units of the scale a sum stays below 2^30.
+constexpr int kRelItemBits = 23;
+// A sum in units of an item's scale as one in units of the head's
+__device__ __forceinline__ long long rel_shifted(int v, int shift) {
+  return shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63);
+}
+
+constexpr int kTwoPerSm = (228 * 1024 - 2 * 1024) / 2 / 16 * 16;  // shared memory of a CTA of which an SM holds two
+
+// The backward of segments of at most 128 rows in one pass (attn_rel_short.cu), where most are so short and the tables fit
+bool attention_rel_bwd_short_applies(const spa_params& p, int n_seg, const RelView& view);
+int launch_attention_rel_bwd_short(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
+                                   const int32_t* seg, int n_seg, const RelBwd& rel, void* dqkv, float* delta, int32_t* d_status,
+                                   cudaStream_t st);
 int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
                                 float* lse, float* peak, int32_t* d_status, cudaStream_t st);
 int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,

@@ -691,17 +691,6 @@ template <int D, bool kDQ, int kRel = kNoRel> __host__ __device__ constexpr int 
          (kRel != kNoRel ? kBwdPosBytes : 0);
 }
 
-// What the kernels with a bias by relative position are given beside the others' arguments.  shared_bins: the table's gradient is
-// summed in shared memory, item by item; else pair by pair in global memory.
-struct RelBwd {
-  RelView view;
-  RelGrad grad;
-  bool shared_bins;
-};
-// The scale of an item's bins.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
-// with |dS| below 2^kRelItemBits in units of the scale a sum stays below 2^30.
-constexpr int kRelItemBits = 23;
-
 template <int D, bool kDQ, bool kLoop, int kRel>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
@@ -1271,7 +1260,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
         const int shift = range[0];
         for (int i = tid; i < rel.view.entries; i += kBwdThreads) {
           const int v = reinterpret_cast<int*>(bins)[i];
-          if (v != 0) rel_add(rel.grad, h, i, shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63));
+          if (v != 0) rel_add(rel.grad, h, i, rel_shifted(v, shift));
         }
       }
       if (again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
@@ -2018,7 +2007,6 @@ attn_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_c
   }
 }
 
-constexpr int kTwoPerSm = (228 * 1024 - 2 * 1024) / 2 / 16 * 16;  // shared memory of a CTA of which an SM holds two
 constexpr int kOnePerSm = 227 * 1024;
 
 // Which kernel runs the dK / dV pass for head dimension D.
@@ -2037,7 +2025,8 @@ template <int kRel> struct kv_pass<64, kRel> {
 // they may take a whole SM's memory), then the table.
 template <int D, int kRel>
 int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
-               const int32_t* seg, int n_seg, void* dqkv, void* workspace, RelBwd rel, int32_t* d_status, cudaStream_t st) {
+               const int32_t* seg, int n_seg, void* dqkv, void* workspace, RelBwd rel, bool long_only, int32_t* d_status,
+               cudaStream_t st) {
   CUtensorMap tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o;  // own tiles: 128-row boxes; streamed tiles: 64-row boxes
   if (!make_tmap_bf16_2d(&tm_qkv, qkv, 3ull * p.C, p.capacity, 6ull * p.C, D, 128, D * 2) ||
       !make_tmap_bf16_2d(&tm_do, dao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, 128, D * 2) ||
@@ -2083,8 +2072,8 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   // Under SPA_FLAG_ONE_PASS_BWD segments of at most 128 rows go to the one-pass kernel (one CTA per segment and
   // head) and the two passes take the longer ones; otherwise, or with more segments than a grid dimension holds, the
   // two passes take everything.
-  const int skip_short = (kRel == kNoRel && (p.flags & SPA_FLAG_ONE_PASS_BWD) && n_seg >= 1 && n_seg <= 65535) ? 1 : 0;
-  if (skip_short) {
+  const int skip_short = kRel != kNoRel ? (int)long_only : ((p.flags & SPA_FLAG_ONE_PASS_BWD) && n_seg >= 1 && n_seg <= 65535) ? 1 : 0;
+  if (kRel == kNoRel && skip_short) {
     launch_pdl(attn_bwd_short_kernel<D>, dim3(p.H, n_seg), kShortThreads, short_smem_bytes<D>(), st, tm_qkv, tm_do, tm_o, lse,
                seg, n_seg, p.capacity, p.C, scale, (__nv_bfloat16*)dqkv, d_status);
     SPA_CUDA_CHECK_LAUNCH("attn_bwd_short_kernel");
@@ -2150,8 +2139,8 @@ size_t tc_attention_workspace_bytes(const spa_params& p) {
 int launch_attention_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                             const int32_t* seg, int n_seg, void* dqkv, void* workspace, int32_t* d_status,
                             cudaStream_t st) {
-  return p.C / p.H == 64 ? bwd_launch<64, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, d_status, st)
-                         : bwd_launch<32, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, d_status, st);
+  return p.C / p.H == 64 ? bwd_launch<64, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, false, d_status, st)
+                         : bwd_launch<32, kNoRel>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, workspace, RelBwd{}, false, d_status, st);
 }
 
 int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
@@ -2159,14 +2148,21 @@ int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void
                                 int32_t* d_status, cudaStream_t st) {
   const RelBwd rel{view, grad, true};
   const int table = view.pitch * 4;
+  const bool one_pass = attention_rel_bwd_short_applies(p, n_seg, view);  // the segments of at most 128 rows
+  if (one_pass) {
+    const int rc = launch_attention_rel_bwd_short(p, qkv, ao, lse, dao, seg, n_seg, rel, dqkv, delta, d_status, st);
+    if (rc != SPA_OK || p.N <= kShortMax) return rc;  // a segment is of one image: there are no longer ones
+  }
+#define SPA_REL_BWD(D, REL) bwd_launch<D, REL>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, one_pass, d_status, st)
   if (p.C / p.H == 64) {
     if (bwd_smem_bytes<64, true, kRelShared>() + 2 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
-      return bwd_launch<64, kRelShared>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
-    return bwd_launch<64, kRelGlobal>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
+      return SPA_REL_BWD(64, kRelShared);
+    return SPA_REL_BWD(64, kRelGlobal);
   }
   if (bwd_smem_bytes<32, true, kRelShared>() + 2 * table <= kTwoPerSm && bwd_smem_bytes<32, false, kRelShared>() + table <= kTwoPerSm)
-    return bwd_launch<32, kRelShared>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
-  return bwd_launch<32, kRelGlobal>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, d_status, st);
+    return SPA_REL_BWD(32, kRelShared);
+  return SPA_REL_BWD(32, kRelGlobal);
+#undef SPA_REL_BWD
 }
 
 int launch_attention_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,
