@@ -22,6 +22,7 @@ struct Prep {
   float* bias;
   int32_t *pos, *owner, *bad;
   uint32_t* redo;
+  unsigned* counters;
   unsigned long long* acc;
   float* bound;
   int n_seg, capacity, B, N, rows, cols, n_buckets, entries, pitch, C, H;
@@ -40,6 +41,9 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   if (kBwd)
     for (int i = threadIdx.x; i < 2 * a.H; i += kPrepThreads) top[i] = 0u;
   const int Np = packed_rows(a.seg, a.n_seg, a.capacity);
+  if (tid == 0) *a.redo = 0u;
+  if (!kBwd)
+    for (int h = tid; h < a.H; h += all) a.counters[h] = 0u;
   for (int o = tid; o < a.pitch; o += all) {
     const int b = o < a.entries ? a.bucket[o] : 0;
     const bool ok = (unsigned)b < (unsigned)a.n_buckets;
@@ -67,7 +71,6 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   if constexpr (kBwd) {
     for (int i = tid; i < a.n_buckets * a.H; i += all) a.acc[i] = 0ull;
     for (int i = tid; i < a.H; i += all) a.bad[i] = 0;
-    if (tid == 0) *a.redo = 0u;
     __syncthreads();
     // A thread has one chunk of a row, the same one of every row it looks at, and neighbouring lanes the other chunks of its head:
     // whole lines per load, and a maximum per thread.  (A thread per row and head read its line in eight loads, which went to L2
@@ -239,6 +242,7 @@ int launch_prep(const spa_params& p, const spa_rel_bias& r, const Layout& l, cha
   a.owner = (int32_t*)(ws + l.owner);
   a.bad = (int32_t*)(ws + l.bad);
   a.redo = (uint32_t*)(ws + l.redo);
+  a.counters = (unsigned*)(ws + l.bad);  // forward and backward use one or the other
   a.acc = (unsigned long long*)(ws + l.acc);
   a.bound = (float*)(ws + l.bound);
   a.n_seg = n_seg;
@@ -269,7 +273,8 @@ int launch_prep(const spa_params& p, const spa_rel_bias& r, const Layout& l, cha
 }
 
 RelView view(const Layout& l, char* ws) {
-  return RelView{(const int32_t*)(ws + l.pos), (const float*)(ws + l.bias), l.pitch, l.entries, l.center};
+  return RelView{(const int32_t*)(ws + l.pos), (const float*)(ws + l.bias), (unsigned*)(ws + l.bad), (uint32_t*)(ws + l.redo),
+                 l.pitch, l.entries, l.center};
 }
 
 }  // namespace

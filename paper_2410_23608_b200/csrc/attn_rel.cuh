@@ -17,8 +17,18 @@ namespace spa {
 struct RelView {          // what the forward and backward kernels read
   const int32_t* pos;     // [capacity + 128]
   const float* bias;      // [H][pitch]: the table's value of every offset
+  unsigned* counters;     // [H] forward: row tiles of a head that have been drawn
+  uint32_t* redo;         // forward: [1 + 4 H capacity], see rel_fwd_note
   int pitch, entries, center;
 };
+
+// A half of a row of the forward's output that is not finite: {row, head, half}, and the CTA's entry before it (numbers from 1 on; 0:
+// none), of which `last` in shared memory is the last.  The CTA that notes it down forms it again.
+__device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int row, int h, int half) {
+  const uint32_t at = atomicAdd(redo, 1u) + 1u;
+  redo[2 * at - 1] = (uint32_t)row | (uint32_t)h << 20 | (uint32_t)half << 28;
+  redo[2 * at] = atomicExch(last, at);
+}
 
 constexpr int kRelBlocks = kNumSMs;  // CTAs of the kernel that prepares a call, each with its own maxima
 struct RelGrad {

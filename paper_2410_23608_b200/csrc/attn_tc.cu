@@ -80,33 +80,52 @@ template <int D, int kRel = kNoRel> struct FwdSmem {
   static constexpr int kSegStage = kRel == kNoRel ? kFwdSegStage : kSegStageRel;
   static constexpr int kSeg = kXl + 1024;                  // staged segment offsets
   static constexpr int kOrder = kSeg + (kSegStage + 4) * 4;
-  // with a bias: the keys' positions of two tiles, a copy for each quarter's warps, and the tables of two items
+  // with a bias: the keys' positions of two tiles, a copy for each quarter's warps, and the head's table
   static constexpr int kPos = kOrder + (int)sizeof(ItemOrder);
   static constexpr int kTable = kPos + (kRel != kNoRel ? 4 * 2 * kKV * 4 : 0);
   static constexpr int kBytes = kTable + 1024;  // and the alignment of the base
-  static constexpr int bytes(int pitch) { return kBytes + (kRel == kRelShared ? 2 * pitch * 4 : 0); }
+  static constexpr int bytes(int pitch) { return kBytes + (kRel == kRelShared ? pitch * 4 : 0); }
 };
 
-// kN head dimensions from column `col` + `first` on of a row's output from the keys of its segment alone: rare, one key after the
-// other from global memory.
-template <int kN>
-__device__ __noinline__ void rel_row_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, int C, int col, int first, int d, int row, int lo,
-                                           int hi, float scale_log2e, const RelView& rel, int h, float m, float inv_l) {
-  const __nv_bfloat16* q = qkv + (long long)row * 3 * C + col;
-  const float* bias = rel.bias + (long long)h * rel.pitch + rel.center + rel.pos[row];
-  for (int e0 = 0; e0 < kN; e0 += 8) {
-    float acc[8] = {};
-    for (int j = lo; j < hi; ++j) {
-      const __nv_bfloat16 *k = qkv + (long long)j * 3 * C + C + col, *v = k + C + first + e0;
-      float s = 0.f;
-      for (int e = 0; e < d; ++e) s = fmaf(__bfloat162float(q[e]), __bfloat162float(k[e]), s);
-      const float p = ptx::ex2_approx(fmaf(s, scale_log2e, bias[-rel.pos[j]]) - (m == -CUDART_INF_F ? 0.f : m));
+// The rows that this CTA has noted down (see rel_fwd_note), from entry `at` on: a half of a row's output from the keys of its segment
+// alone, by a warp, the keys to its lanes.
+__device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, const int32_t* seg, int n_seg, int Np, int C, int d,
+                                           float scale_log2e, const int32_t* pos, const float* table, int pitch, int center,
+                                           const uint32_t* redo, uint32_t at) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = 0; at != 0u; ++i) {
+    const uint32_t what = redo[2 * at - 1];
+    at = redo[2 * at];
+    if (i % (kFwdThreads / 32) != warp) continue;
+    const int row = what & 0xfffff, h = (what >> 20) & 0xff, first = ((what >> 28) & 1) * (d / 2);
+    const RowSeg s = row_segment(seg, n_seg, Np, row);
+    const __nv_bfloat16* q = qkv + (long long)row * 3 * C + h * d;
+    const float* bias = table + (long long)h * pitch + center + pos[row];
+    auto logit = [&](int j) {
+      const __nv_bfloat16* k = qkv + (long long)j * 3 * C + C + h * d;
+      float v = 0.f;
+      for (int e = 0; e < d; ++e) v = fmaf(__bfloat162float(q[e]), __bfloat162float(k[e]), v);
+      return fmaf(v, scale_log2e, bias[-pos[j]]);
+    };
+    float m = -CUDART_INF_F;
+    for (int j = s.lo + lane; j < s.hi; j += 32) m = fmaxf(m, logit(j));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, __bfloat162float(v[e]), acc[e]);
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (m == -CUDART_INF_F) m = 0.f;
+    for (int e0 = first; e0 < first + d / 2; e0 += 8) {
+      float acc[8] = {}, l = 0.f;
+      for (int j = s.lo + lane; j < s.hi; j += 32) {
+        const float p = ptx::ex2_approx(logit(j) - m);
+        const __nv_bfloat16* v = qkv + (long long)j * 3 * C + 2 * C + h * d + e0;
+        l += p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, __bfloat162float(v[e]), acc[e]);
+      }
+      l = warp_sum(l);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = warp_sum(acc[e]) / l;
+      if (lane == 0) *reinterpret_cast<uint4*>(ao + (long long)row * C + h * d + e0) = Vec16<__nv_bfloat16>::from_float(acc);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= inv_l;
-    *reinterpret_cast<uint4*>(ao + (long long)row * C + col + first + e0) = Vec16<__nv_bfloat16>::from_float(acc);
   }
 }
 
@@ -119,8 +138,9 @@ __device__ __noinline__ void rel_row_again(const __nv_bfloat16* qkv, __nv_bfloat
 // 128 segments of 98 to 196 rows, 12 heads of 64: 54 -> 51; one segment of 98 rows: 6.0 us, as before.
 //
 // kRel: S gets a bias by relative position, in units of log 2.  A tile's keys come as positions in shared memory; a pair's bias is
-// then one subtraction and one look-up in the head's table, which the issuing warp fetches an item ahead (kRelShared), or in
-// global memory where two tables do not fit.
+// then one subtraction and one look-up in the head's table, in shared memory (kRelShared) or, where that is too small, in global
+// memory.  All items of a CTA are of one head, so that its table is fetched once; the row tiles of a head are drawn from a counter
+// of its own.
 template <int D, int kRel>
 __global__ void __launch_bounds__(kFwdThreads, 2)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, int n_seg, int capacity,
@@ -157,8 +177,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   float* xl = reinterpret_cast<float*>(smem_al + SM::kXl);
   int32_t* seg_s = reinterpret_cast<int32_t*>(smem_al + SM::kSeg);
   ItemOrder* order = reinterpret_cast<ItemOrder*>(smem_al + SM::kOrder);
-  auto bar_table = [&](int item) { return bar + 200 + 16 * (item & 1); };  // the table of the item has landed; between the item slots
-  auto table_s = [&](int item) { return smem_base + SM::kTable + (item & 1) * rel.pitch * 4; };
+  const uint32_t bar_table = bar + 200, redo_first = bar + 216;  // the table has landed; the last row noted down (between the item slots)
+  const uint32_t table_s = smem_base + SM::kTable;
 
   // The thread that sets the barriers up belongs to the warp that later issues the copies counted on them.
   if (tid == kSoftmaxThreads) {
@@ -167,8 +187,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       ptx::mbar_init(bar_item(b), 1);
       ptx::mbar_init(bar_k(b), 1);
       ptx::mbar_init(bar_v(b), 1);
-      if (kRel == kRelShared) ptx::mbar_init(bar_table(b), 1);
     }
+    if (kRel == kRelShared) ptx::mbar_init(bar_table, 1);
+    if (kRel != kNoRel) ptx::sts_s32(redo_first, 0);
     ptx::mbar_init(bar_q, 1);
     ptx::mbar_init(bar_s, 1);
     ptx::mbar_init(bar_o, 1);
@@ -189,7 +210,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   // Items are drawn behind the whole row tiles that the CTAs start with; longest first where their lengths differ, where
   // they are few enough to be put in order, and where CTAs take 1.5 of them or more (below that, who ends first takes
   // the rest: with 300 to 320 items for 296 CTAs the order cost 3 %, with 432 it was even, with 576 it gained 6 %).
-  const bool draws = counter != nullptr && n_items > (int)gridDim.x;
+  const bool draws = (kRel != kNoRel || counter != nullptr) && n_items > (int)gridDim.x;
   const int given = draws ? (int)gridDim.x / H * H : n_items;
   const bool ordered = !even_items && draws && staged && 2 * n_items >= 3 * (int)gridDim.x && row_tiles - given / H <= kMaxOrder;
   // The issuing warp gets the key rows of the CTA's first item straight from the offsets, of which a lane takes a few,
@@ -235,24 +256,28 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
     // one whose K tile is loaded next, which draws the items.
     struct Cursor { int item, t, n_tiles, h, kv0, q0; };  // item number of this CTA, tile of it; n_tiles 0: past the end
     int own = blockIdx.x, drawn = blockIdx.x;             // static stride without a counter; a number drawn a tile ahead
+    auto draw = [&]() {
+      if constexpr (kRel != kNoRel) {  // the grid is a multiple of H: the numbers stay with the CTA's head
+        own += gridDim.x;
+        const int head = (int)blockIdx.x % H;
+        return draws ? (given / H + (int)atomicAdd(rel.counters + head, 1u)) * H + head : own;
+      } else {
+        return draw_item(counter, given, n_items, own);
+      }
+    };
+    if (kRel == kRelShared) {
+      if (ptx::elect_one()) {
+        ptx::mbar_expect_tx(bar_table, rel.pitch * 4);
+        ptx::bulk_load(table_s, rel.bias + (long long)((int)blockIdx.x % H) * rel.pitch, rel.pitch * 4, bar_table);
+      }
+      __syncwarp();
+    }
     if (draws && (int)blockIdx.x >= given) {
-      if (lane == 0) drawn = draw_item(counter, given, n_items, own);
+      if (lane == 0) drawn = draw();
     }
     bool order_ready = false;
     bool more = true;                                     // numbers are drawn until one lies past the last item
-    int tables = 0;                                       // items whose table has been asked for
     auto announce = [&](const Cursor& c) {
-      if constexpr (kRel == kRelShared) {
-        // its memory: the softmax warps are through with the tables of all items that are two behind this one (see bar_sfree)
-        if (c.n_tiles > 0) {
-          if (ptx::elect_one()) {
-            ptx::mbar_expect_tx(bar_table(c.item), rel.pitch * 4);
-            ptx::bulk_load(table_s(c.item), rel.bias + (long long)c.h * rel.pitch, rel.pitch * 4, bar_table(c.item));
-          }
-          tables = c.item + 1;
-        }
-        __syncwarp();
-      }
       if (lane == 0) {
         const uint32_t slot = item_slot(c.item);
         ptx::sts_s32(slot, c.q0);
@@ -263,7 +288,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
         ptx::sts_s32(slot + 68, Np - c.q0);
         ptx::mbar_arrive(bar_item(c.item & 1));
         // the next number, a tile before it is needed
-        if (c.n_tiles == 1) drawn = draw_item(counter, given, n_items, own);
+        if (c.n_tiles == 1) drawn = draw();
       }
     };
     auto next_item = [&](Cursor& c) {
@@ -312,7 +337,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
     auto advance = [&](Cursor& c) {
       if (++c.t < c.n_tiles) {
         c.kv0 += kKV;
-        if (c.t == c.n_tiles - 1 && lane == 0) drawn = draw_item(counter, given, n_items, own);
+        if (c.t == c.n_tiles - 1 && lane == 0) drawn = draw();
       } else {
         next_item(c);
       }
@@ -414,9 +439,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       for (int i = gv > 2 ? gv - 2 : 0; i < gv; ++i) ptx::mbar_wait(bar_v(i & 1), (i >> 1) & 1);
       for (int i = gk > 2 ? gk - 2 : 0; i < gk; ++i) ptx::mbar_wait(bar_k(i & 1), (i >> 1) & 1);
       if (q_item >= 0) ptx::mbar_wait(bar_q, q_item & 1);
-      if (kRel == kRelShared)
-        for (int i = tables > 2 ? tables - 2 : 0; i < tables; ++i) ptx::mbar_wait(bar_table(i), (i >> 1) & 1);
-      while (more && draws && drawn < n_items) drawn = draw_item(counter, given, n_items, own);
+      if (kRel == kRelShared) ptx::mbar_wait(bar_table, 0);
+      while (more && draws && drawn < n_items) drawn = draw();
     }
     __syncwarp();
   } else {
@@ -456,8 +480,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
         ptx::sts_2s32(pos_q + (g & 1) * kKV * 4 + 8 * (half * 32 + lane), -4 * k0, -4 * k1);
         bias_at = 4 * (rel.center + own);
         if constexpr (kRel == kRelShared) {
-          bias_at += table_s(it);
-          wait(bar_table(it), (it >> 1) & 1);
+          bias_at += table_s;
+          if (it == 0) wait(bar_table, 0);
         } else {
           bias_g = reinterpret_cast<const char*>(rel.bias + (long long)ptx::lds_s32(item_slot(it) + 4) * rel.pitch);
         }
@@ -635,9 +659,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
                     (reinterpret_cast<uintptr_t>(ao) & 31u) == 0);  // rows and heads are whole sectors then
       }
       if constexpr (kRel != kNoRel) {
-        // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, from their own keys
-        __syncwarp();
-        if (again) rel_row_again<kDh>(qkv, ao, C, h * D, half * kDh, D, row, mine.lo, mine.hi, scale_log2e, rel, h, m, inv_l);
+        // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, at the end
+        if (again) rel_fwd_note(rel.redo, reinterpret_cast<uint32_t*>(smem_al + SM::kBar + 216), row, h, half);
       }
       if (half == 0 && rl < rows) {
         lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
@@ -652,6 +675,10 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   if (warp == 0) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem, kTmemCols);
+  }
+  if constexpr (kRel != kNoRel) {
+    const uint32_t at = (uint32_t)ptx::lds_s32(redo_first);
+    if (at != 0u) rel_fwd_again(qkv, ao, seg, n_seg, Np, C, D, scale_log2e, rel.pos, rel.bias, rel.pitch, rel.center, rel.redo, at);
   }
 }
 
@@ -2103,13 +2130,14 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
   if (ea != cudaSuccess) { set_cuda_error(ea, "attn_fwd_tc_kernel"); return SPA_ERR_CUDA; }
   // a persistent grid: two CTAs per SM (at most 94 KB of shared memory, 256 TMEM columns each), never more than work items
   const long long items = (long long)p.H * ((p.capacity + kQ - 1) / kQ);
-  const int grid = (int)(items < 2 * kNumSMs ? items : 2 * kNumSMs);
+  const int most = kRel == kNoRel ? 2 * kNumSMs : 2 * kNumSMs / p.H * p.H;
+  const int grid = (int)(items < most ? items : most);
   // Short segments make items of nearly the same length: putting them in order gained nothing up to segment slots of
   // 400 rows (and cost 1 us in front of short items), and 8 to 12 % from 576 rows on.
   const bool even_items = (long long)p.capacity <= 512ll * (n_seg > 0 ? n_seg : 1);
   launch_pdl(kern, grid, kFwdThreads, smem, st, tm, seg, n_seg, p.capacity, p.C, p.H,
              softmax_scale_of(p) * 1.4426950408889634f, rel, (const __nv_bfloat16*)qkv, (__nv_bfloat16*)ao, lse, peak,
-             items > grid ? item_counter(ao) : nullptr, even_items, d_status);
+             kRel == kNoRel && items > grid ? item_counter(ao) : nullptr, even_items, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_fwd_tc_kernel");
   return SPA_OK;
 }
