@@ -32,7 +32,7 @@ constexpr int kMaxChunks = 1024;  // 16-byte chunks of a row: 8 192 bf16 or 4 09
 constexpr int kSums = 4;          // running sums per channel of the backward: A, B, sum dn yh, sum dn
 // Rows that a CTA has under way with W warps to a row, and its threads.  Backward: one CTA per SM, whose sums are one line to join.
 __host__ __device__ constexpr int groups_of(int W, bool bwd) {
-  return bwd ? (W == 1 ? 16 : W == 2 ? 8 : W == 3 ? 5 : W == 4 ? 4 : W <= 8 ? 16 / W : 1) : (W == 1 ? 8 : W == 2 ? 4 : W == 3 ? 3 : W <= 6 ? 2 : 1);
+  return bwd ? (W == 1 ? 12 : W == 2 ? 6 : W == 3 ? 4 : W == 4 ? 3 : W <= 8 ? 2 : 1) : (W == 1 ? 8 : W == 2 ? 4 : W == 3 ? 3 : W <= 6 ? 2 : 1);
 }
 __host__ __device__ constexpr int threads_of(int W, bool bwd) { return 32 * W * groups_of(W, bwd); }
 
@@ -63,14 +63,14 @@ __device__ __forceinline__ uint4 lds16(uint32_t at) {
 __device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-template <int kA, int kCh, int kDepth, int kThreads> struct Ring {
-  static constexpr int kSlot = kA * kCh * kThreads * 16, kScalars = kThreads / 32 * 32;
+template <int kA, int kCh, int kDepth, int kThreads, int kRows = 1> struct Ring {
+  static constexpr int kSlot = kA * kCh * kThreads * 16, kScalars = kThreads / 32 * 32 * kRows;  // kA: of all kRows rows of a slot
   static constexpr int kBytes = kDepth * (kSlot + kScalars);
   uint32_t base, at, scalar;  // addresses in shared memory: the ring's, this thread's first chunk and its warp's scalars of the slot
   __device__ __forceinline__ explicit Ring(uint32_t b) : base(b) { rewind(); }
   __device__ __forceinline__ void rewind() {
     at = base + threadIdx.x * 16;
-    scalar = base + kDepth * kSlot + (threadIdx.x >> 5) * 32;
+    scalar = base + kDepth * kSlot + (threadIdx.x >> 5) * 32 * kRows;
   }
   __device__ __forceinline__ void next() {
     at += kSlot;
@@ -85,11 +85,11 @@ template <int kA, int kCh, int kDepth, int kThreads> struct Ring {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scalar + 4 * i), "l"(__cvta_generic_to_global(from)) : "memory");
   }
   __device__ __forceinline__ uint4 get(int array, int k) const { return lds16(at + array * kArray + k * kChunk); }
-  __device__ __forceinline__ float4 scalars() const {
-    const uint4 v = lds16(scalar);
+  __device__ __forceinline__ float4 scalars(int row = 0) const {  // eight floats a row
+    const uint4 v = lds16(scalar + 32 * row);
     return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
   }
-  __device__ __forceinline__ float fifth() const { return ptx::lds_f32(scalar + 16); }
+  __device__ __forceinline__ float fifth(int row) const { return ptx::lds_f32(scalar + 32 * row + 16); }
   // Chunks past the end of a row are never copied: they are read as zeros, like the others, when they have been cleared once.
   __device__ __forceinline__ void clear(int t0, int stride, int Q) {
     for (int slot = 0; slot < kDepth; ++slot, next())
@@ -102,43 +102,52 @@ template <int kA, int kCh, int kDepth, int kThreads> struct Ring {
   }
 };
 
-// Sums of kN values over the group's threads, in every one of them.  Calls alternate between two lines: a warp that
-// writes a line again has met the others at the barrier in between, behind their reads of it.
+// Sums of kN values over the group's threads, in every one of them.  Two or four values go through a warp together: each step
+// leaves every lane half of the values it had, so that 6 shuffles serve four values instead of 20.  Calls alternate between two
+// lines of shared memory: a warp that writes a line again has met the others at the barrier in between, behind their reads of it.
 template <int W> struct GroupSum {
-  uint32_t line, other;  // [W][4] floats of this group each, in shared memory
+  uint32_t line, other;  // [W][8] floats of this group each
   int id, warp, lane;
   template <int kN> __device__ __forceinline__ void operator()(float (&v)[kN]) {
-    static_assert(kN <= 3, "a line has room for four");
-    // two values at once: half of the lanes carries each of them through the last four steps
-    if constexpr (kN >= 2) {
-      const bool up = (lane & 16) != 0;
-      float s = up ? v[1] : v[0];
-      s += __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
+    static_assert(kN <= 4 || kN == 6, "a line has room for eight, in fours, twos and ones");
+    if constexpr (W == 1 && kN == 1) {
+      v[0] = warp_sum(v[0]);
+    } else {
+      const uint32_t mine = line + 32 * warp;
+      constexpr int k4 = kN / 4 * 4, k2 = (kN - k4) / 2 * 2;
+      if constexpr (k4 == 4) {
+        const bool up = (lane & 16) != 0, up8 = (lane & 8) != 0;
+        float a = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
+        float b = (up ? v[3] : v[2]) + __shfl_xor_sync(0xffffffffu, up ? v[2] : v[3], 16);
+        a = (up8 ? b : a) + __shfl_xor_sync(0xffffffffu, up8 ? a : b, 8);
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      v[0] = v[1] = s;
-      if constexpr (W == 1) {
-        const float t = __shfl_xor_sync(0xffffffffu, s, 16);
-        v[0] = up ? t : s;
-        v[1] = up ? s : t;
+        for (int o = 4; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        if ((lane & 7) == 0) ptx::sts_s32(mine + 4 * ((lane >> 4) + ((lane >> 2) & 2)), __float_as_int(a));
       }
-    }
-    if constexpr (kN != 2) {
+      if constexpr (k2 == 2) {
+        const bool up = (lane & 16) != 0;
+        float a = (up ? v[k4 + 1] : v[k4]) + __shfl_xor_sync(0xffffffffu, up ? v[k4] : v[k4 + 1], 16);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v[kN - 1] += __shfl_xor_sync(0xffffffffu, v[kN - 1], o);
-    }
-    if constexpr (W > 1) {
-      const uint32_t mine = line + 16 * warp;
-      if (lane == 0) ptx::sts_s32(mine, __float_as_int(v[0]));
-      if (kN >= 2 && lane == 16) ptx::sts_s32(mine + 4, __float_as_int(v[1]));
-      if (kN == 3 && lane == 0) ptx::sts_s32(mine + 8, __float_as_int(v[2]));
-      asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "n"(32 * W) : "memory");
+        for (int o = 8; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        if ((lane & 15) == 0) ptx::sts_s32(mine + 4 * (k4 + (lane >> 4)), __float_as_int(a));
+      }
+      if constexpr (kN - k4 - k2 == 1) {
+        const float a = warp_sum(v[kN - 1]);
+        if (lane == 0) ptx::sts_s32(mine + 4 * (kN - 1), __float_as_int(a));
+      }
+      if constexpr (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "n"(32 * W) : "memory");
+      else __syncwarp();
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const uint4 l = lds16(line + 16 * w);
-        v[0] = w == 0 ? __uint_as_float(l.x) : v[0] + __uint_as_float(l.x);
-        if (kN >= 2) v[1] = w == 0 ? __uint_as_float(l.y) : v[1] + __uint_as_float(l.y);
-        if (kN == 3) v[2] = w == 0 ? __uint_as_float(l.z) : v[2] + __uint_as_float(l.z);
+        const uint4 l = lds16(line + 32 * w);
+        float f[8] = {__uint_as_float(l.x), __uint_as_float(l.y), __uint_as_float(l.z), __uint_as_float(l.w)};
+        if constexpr (kN > 4) {
+          const uint4 m = lds16(line + 32 * w + 16);
+          f[4] = __uint_as_float(m.x);
+          f[5] = __uint_as_float(m.y);
+        }
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = w == 0 ? f[i] : v[i] + f[i];
       }
       const uint32_t t = line;
       line = other;
@@ -202,10 +211,10 @@ template <typename T, int W, int kCh, int kGate>
 __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / threads_of(W, false) : 1) sandwich_fwd_kernel(const Args a) {
   pdl_entry();
   constexpr int P = kPairs<T>, G = 32 * W;
-  __shared__ __align__(16) float red[groups_of(W, false) * 8 * W];
+  __shared__ __align__(16) float red[groups_of(W, false) * 16 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  const uint32_t lines = ptx::smem_u32(red + grp * 8 * W);
-  GroupSum<W> sum{lines, lines + 16 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
+  const uint32_t lines = ptx::smem_u32(red + grp * 16 * W);
+  GroupSum<W> sum{lines, lines + 32 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
   const float inv_c = 1.f / a.C;
   const bool layer = a.kind == SPA_NORM_LAYER;
   // y = x + gate (cw zh + cb), n = cp norm(y) + bp
@@ -353,7 +362,12 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
 }
 
 template <int kGate> constexpr int kBwdArrays = kGate == SPA_GATE_TOKEN ? 5 : 4;
-template <int kCh> constexpr int kBwdDepth = kCh == 1 ? 3 : 2;
+// Rows that a group takes together, whose sums share shuffles and barriers: a row's steps depend on one another, and with one at a time
+// 18 432 rows of 768 took 43 us whatever their bytes.  And how many such steps ahead they are copied.
+// Two need 168 registers, so CTAs of 384 threads: 18 432 rows of 768 46.5 -> 44 us, 9 216 of 1 536 51 -> 46; with CTAs of 512 (8 and 16
+// warps to a row) they spill: 8 184 rows of 4 096 109 -> 120.
+template <int W, int kCh> constexpr int kBwdRows = kCh == 1 && W != 8 && W != 16 ? 2 : 1;
+template <int W, int kCh> constexpr int kBwdDepth = kCh == 1 && kBwdRows<W, kCh> == 1 ? 3 : 2;
 
 // A CTA has a share of the rows, one behind the other.  With a gate per image the sums A_b and B_b leave it at the end of each image
 // or share: the line of image b from CTA c is line b + c, since one of the two goes up from each to the next.
@@ -362,16 +376,16 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
   pdl_entry();
   constexpr int P = kPairs<T>, G = 32 * W, kG = groups_of(W, true);
   constexpr bool kImage = kGate == SPA_GATE_IMAGE;
-  constexpr int kDepth = kBwdDepth<kCh>;
-  using Rows = Ring<kBwdArrays<kGate>, kCh, kDepth, threads_of(W, true)>;
+  constexpr int kDepth = kBwdDepth<W, kCh>, R = kBwdRows<W, kCh>, kStep = kG * R;
+  using Rows = Ring<kBwdArrays<kGate> * R, kCh, kDepth, threads_of(W, true), R>;
   // the ring, and in its place, when it is empty, [kG][2][C] sums; behind them, with a gate per image, [2][C]: sum of gate_b A_b,
   // of gate_b B_b
   extern __shared__ __align__(16) uint8_t smem[];
   float* acc_s = reinterpret_cast<float*>(smem);
-  __shared__ __align__(16) float red[kG * 8 * W];
+  __shared__ __align__(16) float red[kG * 16 * W];
   const int grp = threadIdx.x / G, t0 = threadIdx.x % G;
-  const uint32_t lines = ptx::smem_u32(red + grp * 8 * W);
-  GroupSum<W> sum{lines, lines + 16 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
+  const uint32_t lines = ptx::smem_u32(red + grp * 16 * W);
+  GroupSum<W> sum{lines, lines + 32 * W, grp, t0 >> 5, (int)threadIdx.x & 31};
   const float inv_c = 1.f / a.C;
   const bool layer = a.kind == SPA_NORM_LAYER;
   uint64_t sA[kCh][P] = {}, sB[kCh][P] = {}, sG[kCh][P] = {}, sN[kCh][P] = {};
@@ -424,7 +438,6 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 #pragma unroll
   for (int k = 0; k < kCh; ++k) param<T>(a.g_pre, t0 + G * k, t0 + G * k < a.Q, 1.f, cp[k]);
   if (!kImage) products(nullptr);
-  struct Row { uint4 n[kCh], y[kCh], d[kCh], z[kCh], g[kGate == SPA_GATE_TOKEN ? kCh : 1]; float m1, r1, m2, r2, score; int zr; };
   Rows ring(ptx::smem_u32(smem));
   auto has_row = [&](int zr) { return zr >= 0 && zr < a.z_rows; };
   const int share = blockIdx.x * a.rows_per_cta, share_end = share + a.rows_per_cta < a.rows ? share + a.rows_per_cta : a.rows;
@@ -433,171 +446,213 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
     end = kImage && (image + 1) * a.N < share_end ? (image + 1) * a.N : share_end;
     if (kImage) products(static_cast<const uint4*>(a.gate) + (long long)image * a.Q);
     auto row_of = [&](int t) { return a.z_row != nullptr && t < end ? ld_dep(a.z_row + t) : t; };
-    auto fetch = [&](int t, int zr) {
-      if (t < end) {
-        const bool has = has_row(zr);
-        const unsigned at = t * a.Q + t0, zat = zr * a.Q + t0;  // places in chunks: below 2^30
+    auto fetch = [&](int t, const int (&zr)[R]) {
+#pragma unroll
+      for (int r = 0; r < R; ++r, t += kG) {
+        if (t >= end) continue;
+        const bool has = has_row(zr[r]);
+        const unsigned at = t * a.Q + t0, zat = zr[r] * a.Q + t0;  // places in chunks: below 2^30
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
           if (t0 + G * k < a.Q) {
             if (a.dn != nullptr) {
-              ring.copy(0, k, a.dn + (at + G * k));
-              ring.copy(1, k, a.y + (at + G * k));
+              ring.copy(r, k, a.dn + (at + G * k));
+              ring.copy(R + r, k, a.y + (at + G * k));
             }
-            if (a.dy != nullptr) ring.copy(2, k, a.dy + (at + G * k));
+            if (a.dy != nullptr) ring.copy(2 * R + r, k, a.dy + (at + G * k));
             if (has) {
-              ring.copy(3, k, a.z + (zat + G * k));
-              if (kGate == SPA_GATE_TOKEN) ring.copy(kGate == SPA_GATE_TOKEN ? 4 : 0, k, static_cast<const uint4*>(a.gate) + (at + G * k));
+              ring.copy(3 * R + r, k, a.z + (zat + G * k));
+              if (kGate == SPA_GATE_TOKEN) ring.copy(kGate == SPA_GATE_TOKEN ? 4 * R + r : 0, k, static_cast<const uint4*>(a.gate) + (at + G * k));
             }
           }
         }
-        if (sum.lane < 4) ring.copy_scalar(sum.lane, a.stats + (unsigned)(sum.lane * a.rows + t));
-        if (kGate == SPA_GATE_SCORE && sum.lane == 4) ring.copy_scalar(4, static_cast<const float*>(a.gate) + t);
+        if (sum.lane < 4) ring.copy_scalar(8 * r + sum.lane, a.stats + (unsigned)(sum.lane * a.rows + t));
+        if (kGate == SPA_GATE_SCORE && sum.lane == 4) ring.copy_scalar(8 * r + 4, static_cast<const float*>(a.gate) + t);
       }
       cp_async_commit();
     };
     ring.clear(t0, G, a.Q);
-    int t = begin + grp, zr[kDepth + 1];  // rows of z of the tokens on their way, and of one more
+    int t = begin + grp, zr[kDepth + 1][R];  // rows of z of the tokens on their way, and of the next ones
 #pragma unroll
-    for (int i = 0; i <= kDepth; ++i) zr[i] = row_of(t + i * kG);
+    for (int i = 0; i <= kDepth; ++i)
+#pragma unroll
+      for (int r = 0; r < R; ++r) zr[i][r] = row_of(t + i * kStep + r * kG);
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) {
-      fetch(t + i * kG, zr[i]);
+      fetch(t + i * kStep, zr[i]);
       ring.next();
     }
-    for (; t < end; t += kG) {
+    for (; t < end; t += kStep) {
       cp_async_wait<kDepth - 1>();
       __syncwarp();
-      Row cur;
-      {
-        cur.zr = has_row(zr[0]) ? zr[0] : -1;
+      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+      uint4 nr[R][kCh], yr[R][kCh], dr[R][kCh], zv[R][kCh], gr[R][kGate == SPA_GATE_TOKEN ? kCh : 1];
+      float m1[R], r1[R], m2[R], r2[R], score[R];
+      bool has[R], there[R];
+      unsigned at[R], zat[R];
 #pragma unroll
-        for (int k = 0; k < kCh; ++k) {  // of absent arrays and rows: what was there, and is not used
-          cur.n[k] = ring.get(0, k);
-          cur.y[k] = ring.get(1, k);
-          cur.d[k] = a.dy != nullptr ? ring.get(2, k) : make_uint4(0u, 0u, 0u, 0u);
-          cur.z[k] = ring.get(3, k);
-          if constexpr (kGate == SPA_GATE_TOKEN) cur.g[k] = ring.get(4, k);
-        }
-        const float4 sc = ring.scalars();
-        cur.m1 = sc.x;
-        cur.r1 = sc.y;
-        cur.m2 = sc.z;
-        cur.r2 = sc.w;
-        cur.score = kGate == SPA_GATE_SCORE ? ring.fifth() : 0.f;
-      }
-      __syncwarp();
-      fetch(t + kDepth * kG, zr[kDepth]);
-      ring.next();
-#pragma unroll
-      for (int i = 0; i < kDepth; ++i) zr[i] = zr[i + 1];
-      zr[kDepth] = row_of(t + (kDepth + 1) * kG);
-      const unsigned at = t * a.Q + t0, zat = cur.zr * a.Q + t0;
-      const bool has = cur.zr >= 0;
-      // ---- through the norm behind the sum: d, the gradient of y
-      uint64_t d[kCh][P];
-      if (a.dn != nullptr) {
-        const uint64_t r = both(cur.r2), m = both(-cur.m2 * cur.r2);
-        uint64_t s1 = 0ull, s2 = 0ull, yh[kCh][P];
+      for (int r = 0; r < R; ++r) {
+        there[r] = r == 0 || t + r * kG < end;
+        has[r] = there[r] && has_row(zr[0][r]);
+        at[r] = (t + r * kG) * a.Q + t0;
+        zat[r] = zr[0][r] * a.Q + t0;
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
-          uint64_t n[P];
-          to_pairs(cur.n[k], n);
-          to_pairs(cur.y[k], yh[k]);
+          nr[r][k] = ring.get(r, k);
+          yr[r][k] = ring.get(R + r, k);
+          dr[r][k] = ring.get(2 * R + r, k);
+          zv[r][k] = ring.get(3 * R + r, k);
+          if constexpr (kGate == SPA_GATE_TOKEN) gr[r][k] = ring.get(4 * R + r, k);
+        }
+        const float4 sc = ring.scalars(r);
+        m1[r] = sc.x;
+        r1[r] = sc.y;
+        m2[r] = sc.z;
+        r2[r] = sc.w;
+        score[r] = kGate == SPA_GATE_SCORE ? ring.fifth(r) : 0.f;
+        // what was not copied: whatever was there
+        if (!there[r] || a.dn == nullptr) {
+          m2[r] = r2[r] = 0.f;
 #pragma unroll
-          for (int i = 0; i < P; ++i) {  // chunks past the end: n is zero
-            yh[k][i] = fma2(yh[k][i], r, m);
-            sG[k][i] = fma2(n[i], yh[k][i], sG[k][i]);
-            sN[k][i] = add2(sN[k][i], n[i]);
-            d[k][i] = mul2(n[i], cp[k][i]);
-            s1 = add2(s1, d[k][i]);
-            s2 = fma2(d[k][i], yh[k][i], s2);
+          for (int k = 0; k < kCh; ++k) nr[r][k] = yr[r][k] = zero;
+        }
+        if (!there[r] || a.dy == nullptr) {
+#pragma unroll
+          for (int k = 0; k < kCh; ++k) dr[r][k] = zero;
+        }
+        if (!has[r]) {
+          m1[r] = r1[r] = 0.f;
+#pragma unroll
+          for (int k = 0; k < kCh; ++k) {
+            zv[r][k] = zero;
+            if constexpr (kGate == SPA_GATE_TOKEN) gr[r][k] = zero;
           }
         }
-        float s[2] = {sum_of(s1), sum_of(s2)};
+      }
+      __syncwarp();
+      fetch(t + kDepth * kStep, zr[kDepth]);
+      ring.next();
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) zr[i][r] = zr[i + 1][r];
+        zr[kDepth][r] = row_of(t + (kDepth + 1) * kStep + r * kG);
+      }
+      // ---- through the norm behind the sum: d, the gradient of y
+      uint64_t d[R][kCh][P];
+      if (a.dn != nullptr) {
+        uint64_t yh[R][kCh][P];
+        float s[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const uint64_t rs = both(r2[r]), m = both(-m2[r] * r2[r]);
+          uint64_t s1 = 0ull, s2 = 0ull;
+#pragma unroll
+          for (int k = 0; k < kCh; ++k) {
+            uint64_t n[P];
+            to_pairs(nr[r][k], n);
+            to_pairs(yr[r][k], yh[r][k]);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {  // chunks past the end: n is zero
+              yh[r][k][i] = fma2(yh[r][k][i], rs, m);
+              sG[k][i] = fma2(n[i], yh[r][k][i], sG[k][i]);
+              sN[k][i] = add2(sN[k][i], n[i]);
+              d[r][k][i] = mul2(n[i], cp[k][i]);
+              s1 = add2(s1, d[r][k][i]);
+              s2 = fma2(d[r][k][i], yh[r][k][i], s2);
+            }
+          }
+          s[2 * r] = sum_of(s1);
+          s[2 * r + 1] = sum_of(s2);
+        }
         sum(s);
         // d = dy + (g - mean g - yh mean(g yh)) / deviation
-        const uint64_t a1 = both(layer ? -s[0] * inv_c * cur.r2 : 0.f), a2 = both(-s[1] * inv_c * cur.r2);
 #pragma unroll
-        for (int k = 0; k < kCh; ++k) {
-          uint64_t y[P];
-          to_pairs(cur.d[k], y);
+        for (int r = 0; r < R; ++r) {
+          const uint64_t rs = both(r2[r]), a1 = both(layer ? -s[2 * r] * inv_c * r2[r] : 0.f), a2 = both(-s[2 * r + 1] * inv_c * r2[r]);
 #pragma unroll
-          for (int i = 0; i < P; ++i) d[k][i] = add2(y[i], fma2(d[k][i], r, fma2(yh[k][i], a2, a1)));
+          for (int k = 0; k < kCh; ++k) {
+            uint64_t y[P];
+            to_pairs(dr[r][k], y);
+#pragma unroll
+            for (int i = 0; i < P; ++i) d[r][k][i] = add2(y[i], fma2(d[r][k][i], rs, fma2(yh[r][k][i], a2, a1)));
+          }
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < kCh; ++k) to_pairs(cur.d[k], d[k]);
-      }
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int k = 0; k < kCh; ++k)
-        if (t0 + G * k < a.Q) a.dx[at + G * k] = from_pairs(d[k]);
-      if (has) {
-        const float score = kGate == SPA_GATE_SCORE ? sigmoid(cur.score) : 1.f;
-        const uint64_t r = both(cur.r1), m = both(-cur.m1 * cur.r1), w = both(score);
-        uint64_t u1 = 0ull, u2 = 0ull, u3 = 0ull, zh[kCh][P];
+          for (int k = 0; k < kCh; ++k) to_pairs(dr[r][k], d[r][k]);
+      }
+      // ---- through gate, scale and the norm in front of the sum
+      constexpr int kU = kGate == SPA_GATE_SCORE ? 3 : 2;
+      uint64_t zh[R][kCh][P];
+      float u[kU * R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (kGate == SPA_GATE_SCORE) score[r] = sigmoid(score[r]);
+        const uint64_t rs = both(r1[r]), m = both(-m1[r] * r1[r]), w = both(score[r]);
+        uint64_t u1 = 0ull, u2 = 0ull, u3 = 0ull;
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
           const bool in = t0 + G * k < a.Q;
+          if (in && there[r]) a.dx[at[r] + G * k] = from_pairs(d[r][k]);
           uint64_t g[P];
-          to_pairs(cur.z[k], zh[k]);
-          if constexpr (kGate == SPA_GATE_TOKEN) to_pairs(cur.g[k], g);
+          to_pairs(zv[r][k], zh[r][k]);
+          if constexpr (kGate == SPA_GATE_TOKEN) to_pairs(gr[r][k], g);
 #pragma unroll
           for (int i = 0; i < P; ++i) {
-            if (!in) d[k][i] = 0ull;  // the means' part
-            zh[k][i] = fma2(zh[k][i], r, m);
-            if (kGate == SPA_GATE_SCORE) u3 = fma2(d[k][i], fma2(zh[k][i], cw[k][i], cb[k][i]), u3);
+            if (!in || !has[r]) d[r][k][i] = 0ull;  // past the end: the means' part; without a row: nothing
+            zh[r][k][i] = fma2(zh[r][k][i], rs, m);
+            if (kGate == SPA_GATE_SCORE) u3 = fma2(d[r][k][i], fma2(zh[r][k][i], cw[k][i], cb[k][i]), u3);
             if constexpr (kGate == SPA_GATE_TOKEN) {
-              const uint64_t dg = mul2(d[k][i], fma2(zh[k][i], cw[k][i], cb[k][i]));
-              d[k][i] = mul2(d[k][i], g[i]);
+              const uint64_t dg = mul2(d[r][k][i], fma2(zh[r][k][i], cw[k][i], cb[k][i]));
+              d[r][k][i] = mul2(d[r][k][i], g[i]);
               g[i] = dg;
             }
-            if (kGate == SPA_GATE_SCORE) d[k][i] = mul2(d[k][i], w);
-            sA[k][i] = fma2(d[k][i], zh[k][i], sA[k][i]);
-            sB[k][i] = add2(sB[k][i], d[k][i]);
-            d[k][i] = mul2(d[k][i], cw[k][i]);  // gz
-            u1 = add2(u1, d[k][i]);
-            u2 = fma2(d[k][i], zh[k][i], u2);
+            if (kGate == SPA_GATE_SCORE) d[r][k][i] = mul2(d[r][k][i], w);
+            sA[k][i] = fma2(d[r][k][i], zh[r][k][i], sA[k][i]);
+            sB[k][i] = add2(sB[k][i], d[r][k][i]);
+            d[r][k][i] = mul2(d[r][k][i], cw[k][i]);  // gz
+            u1 = add2(u1, d[r][k][i]);
+            u2 = fma2(d[r][k][i], zh[r][k][i], u2);
           }
           if constexpr (kGate == SPA_GATE_TOKEN) {
-            if (in && a.dgate != nullptr) {
+            if (in && there[r] && a.dgate != nullptr) {
               if (a.gate_f32) {
 #pragma unroll
                 for (int i = 0; i < P; i += 2)
-                  static_cast<ulonglong2*>(a.dgate)[(size_t)(at + G * k) * (P / 2) + i / 2] = make_ulonglong2(g[i], g[i + 1]);
+                  static_cast<ulonglong2*>(a.dgate)[(size_t)(at[r] + G * k) * (P / 2) + i / 2] = make_ulonglong2(g[i], g[i + 1]);
               } else {
-                static_cast<uint4*>(a.dgate)[at + G * k] = from_pairs(g);
+                static_cast<uint4*>(a.dgate)[at[r] + G * k] = from_pairs(g);
               }
             }
           }
         }
-        float s[kGate == SPA_GATE_SCORE ? 3 : 2];
-        s[0] = sum_of(u1);
-        s[1] = sum_of(u2);
-        if constexpr (kGate == SPA_GATE_SCORE) s[2] = sum_of(u3);
-        sum(s);
+        u[2 * r] = sum_of(u1);
+        u[2 * r + 1] = sum_of(u2);
+        if constexpr (kGate == SPA_GATE_SCORE) u[2 * R + r] = sum_of(u3);
+      }
+      bool any = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) any = any || has[r];
+      if (any) sum(u);  // the same for the whole group
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
         if constexpr (kGate == SPA_GATE_SCORE) {
-          if (t0 == 0 && a.dgate != nullptr) static_cast<float*>(a.dgate)[t] = s[2] * score * (1.f - score);
+          if (t0 == 0 && there[r] && a.dgate != nullptr)
+            static_cast<float*>(a.dgate)[t + r * kG] = has[r] ? u[2 * R + r] * score[r] * (1.f - score[r]) : 0.f;
         }
-        const uint64_t a1 = both(layer ? -s[0] * inv_c * cur.r1 : 0.f), a2 = both(-s[1] * inv_c * cur.r1);
+        if (has[r]) {
+          const uint64_t rs = both(r1[r]), a1 = both(layer ? -u[2 * r] * inv_c * r1[r] : 0.f), a2 = both(-u[2 * r + 1] * inv_c * r1[r]);
 #pragma unroll
-        for (int k = 0; k < kCh; ++k) {
-          if (t0 + G * k < a.Q) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) d[k][i] = fma2(d[k][i], r, fma2(zh[k][i], a2, a1));
-            a.dz[zat + G * k] = from_pairs(d[k]);
-          }
-        }
-      } else if (a.dgate != nullptr) {
-        if (kGate == SPA_GATE_SCORE && t0 == 0) static_cast<float*>(a.dgate)[t] = 0.f;
-        if (kGate == SPA_GATE_TOKEN) {
-#pragma unroll
-          for (int k = 0; k < kCh; ++k)
+          for (int k = 0; k < kCh; ++k) {
             if (t0 + G * k < a.Q) {
 #pragma unroll
-              for (int i = 0; i < (a.gate_f32 ? P / 2 : 1); ++i)
-                static_cast<uint4*>(a.dgate)[(size_t)(at + G * k) * (a.gate_f32 ? P / 2 : 1) + i] = make_uint4(0u, 0u, 0u, 0u);
+              for (int i = 0; i < P; ++i) d[r][k][i] = fma2(d[r][k][i], rs, fma2(zh[r][k][i], a2, a1));
+              a.dz[zat[r] + G * k] = from_pairs(d[r][k]);
             }
+          }
         }
       }
     }
@@ -733,7 +788,7 @@ template <typename T, int W, int kCh, int kGate> int fwd_launch(const Args& a, c
 
 template <typename T, int W, int kCh, int kGate> int bwd_launch(const Args& a, const Plan& pl, cudaStream_t st) {
   auto kern = sandwich_bwd_kernel<T, W, kCh, kGate>;
-  constexpr int kRing = Ring<kBwdArrays<kGate>, kCh, kBwdDepth<kCh>, threads_of(W, true)>::kBytes;
+  constexpr int kRing = Ring<kBwdArrays<kGate> * kBwdRows<W, kCh>, kCh, kBwdDepth<W, kCh>, threads_of(W, true), kBwdRows<W, kCh>>::kBytes;
   auto bytes = [](int channels) {
     const int acc = groups_of(W, true) * 2 * channels * (int)sizeof(float);
     return (acc > kRing ? acc : kRing) + (kGate == SPA_GATE_IMAGE ? 2 * channels * (int)sizeof(float) : 0);
