@@ -2091,7 +2091,8 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   // three grids' worth of slots stands for one and a half items per CTA or more.
   const long long items = (long long)p.H * ((p.capacity + 127) / 128);
   const bool even_items = (long long)p.capacity <= 256ll * (n_seg > 0 ? n_seg : 1);
-  const bool loop = even_items && items >= 3ll * 2 * kNumSMs;
+  // (Behind the one-pass kernels of a problem with a bias few items are left, often none: a CTA per item cost 12 us of 95 for nothing.)
+  const bool loop = (even_items && items >= 3ll * 2 * kNumSMs) || (kRel != kNoRel && long_only && items >= 2ll * kNumSMs);
   const int grid = (int)(loop ? 2 * kNumSMs : items);
   auto kq = loop ? attn_bwd_tc_kernel<D, true, true, kRel> : attn_bwd_tc_kernel<D, true, false, kRel>;
   auto kkv = loop ? KV::template kernel<true>() : KV::template kernel<false>();
