@@ -105,6 +105,25 @@ __device__ __forceinline__ long long rel_shifted(int v, int shift) {
   return shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63);
 }
 
+// The bins of an item to the head's sums, by kThreads threads: four at a time, so that the look-ups of their buckets do not wait for
+// one another
+template <int kThreads>
+__device__ __forceinline__ void rel_flush(const RelBwd& rel, const int* bins, int h, int shift, int tid) {
+  for (int i = tid; i < rel.view.entries; i += 4 * kThreads) {
+    int v[4], b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int at = i + u * kThreads;
+      v[u] = at < rel.view.entries ? bins[at] : 0;
+      b[u] = v[u] != 0 ? rel.grad.bucket[at] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if ((unsigned)b[u] < (unsigned)rel.grad.n_buckets)
+        atomicAdd(rel.grad.acc + (long long)h * rel.grad.n_buckets + b[u], (unsigned long long)rel_shifted(v[u], shift));
+  }
+}
+
 constexpr int kTwoPerSm = (228 * 1024 - 2 * 1024) / 2 / 16 * 16;  // shared memory of a CTA of which an SM holds two
 
 // The backward of segments of at most 128 rows in one pass (attn_rel_short.cu), where most are so short and the tables fit

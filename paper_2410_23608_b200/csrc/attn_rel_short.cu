@@ -85,16 +85,18 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
   bool failed = false;
   uint32_t parity = 0;
 
+  // the grid is a multiple of H: all of a CTA's items are of one head, whose table and bound it fetches once
+  const int h = blockIdx.x % H;
+  const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
+  for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<float4*>(table)[i] = from[i];
+  float head_v;
+  const int head_exp = rel_exponent(rel_head_bound(rel.grad, h, head_v));
   for (int item = blockIdx.x; item < n_items && !failed; item += gridDim.x) {
-    const int h = item % H, s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
+    const int s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
     if (tid <= count) {
       const int o = ld_dep(seg + s0 + tid);
       seg_s[tid] = o < Np ? o : Np;
     }
-    const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
-    for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<float4*>(table)[i] = from[i];
-    float head_v;
-    const int head_exp = rel_exponent(rel_head_bound(rel.grad, h, head_v));
     __syncthreads();
     int first = 0;
     auto length = [&](int s) { return seg_s[s + 1] - seg_s[s]; };
@@ -304,10 +306,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
         __syncwarp();
       }
       // ---- the tile's bins to the head's sums, under the products
-      for (int i = tid; i < rel.view.entries; i += kThreads) {
-        const int v = reinterpret_cast<const int*>(bins)[i];
-        if (v != 0) rel_add(rel.grad, h, i, rel_shifted(v, bin_shift));
-      }
+      rel_flush<kThreads>(rel, reinterpret_cast<const int*>(bins), h, bin_shift, tid);
       wait(bar_acc, parity);
       ptx::tc_fence_after_sync();
       // ---- dV, dK, dQ rows as bf16 into the Q, K, dO tiles' memory (idle now), from where whole lines go out
@@ -351,7 +350,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
       first = end;
       __syncthreads();
     }
-    __syncthreads();  // the offsets and the table are free for the next segments
+    __syncthreads();  // the offsets' memory is free for the next segments
   }
   if (failed) {  // what is in flight lands before the memory is released
     if (tid == 0) ptx::mbar_wait(bar_ld, parity);
@@ -456,16 +455,18 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
   bool failed = false;
   uint32_t parity = 0;
 
+  // the grid is a multiple of H: all of a CTA's items are of one head, whose table and bound it fetches once
+  const int h = blockIdx.x % H;
+  const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
+  for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<float4*>(table)[i] = from[i];
+  float head_v;
+  const int head_exp = rel_exponent(rel_head_bound(rel.grad, h, head_v));
   for (int item = blockIdx.x; item < n_items && !failed; item += gridDim.x) {
-    const int h = item % H, s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
+    const int s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
     if (tid <= count) {
       const int o = ld_dep(seg + s0 + tid);
       seg_s[tid] = o < Np ? o : Np;
     }
-    const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
-    for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<float4*>(table)[i] = from[i];
-    float head_v;
-    const int head_exp = rel_exponent(rel_head_bound(rel.grad, h, head_v));
     __syncthreads();
     auto length = [&](int s) { return seg_s[s + 1] - seg_s[s]; };
     int next = 0;
@@ -655,10 +656,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
         __syncwarp();
       }
       // ---- the tile's bins to the head's sums, under the products
-      for (int i = tid; i < rel.view.entries; i += kThreads) {
-        const int v = reinterpret_cast<const int*>(bins)[i];
-        if (v != 0) rel_add(rel.grad, h, i, rel_shifted(v, bin_shift));
-      }
+      rel_flush<kThreads>(rel, reinterpret_cast<const int*>(bins), h, bin_shift, tid);
       wait(bar_p, parity);  // dS takes the memory of P
 #pragma unroll
       for (int c = 0; c < 4; ++c)
@@ -734,7 +732,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
       parity ^= 1;
       __syncthreads();
     }
-    __syncthreads();  // the offsets and the table are free for the next segments
+    __syncthreads();  // the offsets' memory is free for the next segments
   }
   if (failed) {  // what is in flight lands before the memory is released
     if (tid == 0) ptx::mbar_wait(bar_ld, parity);
@@ -753,10 +751,10 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
   }
 }
 
-// Segments that a CTA takes at a time: so many that it gets about four items, whose number evens them out; by fours, of which the
+// Segments that a CTA takes at a time: so many that it gets about two items (512 windows of 7 x 7, 12 heads of 32: four 105 us, two 93, one 109); by fours, of which the
 // tiles take two, three or four together.
 int chunk_of(int n_seg, int H, int ctas) {
-  long long chunk = (long long)n_seg * H / (4 * ctas);
+  long long chunk = (long long)n_seg * H / (2 * ctas);
   chunk = chunk < 1 ? 1 : (chunk > kMaxChunk ? kMaxChunk : chunk);
   return (int)(chunk >= 4 ? chunk & ~3ll : chunk);
 }
@@ -773,7 +771,7 @@ int launch_pair(const spa_params& p, const void* qkv, const void* ao, const floa
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PairSmem<D>::kMost); });
   if (ea != cudaSuccess) { set_cuda_error(ea, "rel_bwd_pair_kernel"); return SPA_ERR_CUDA; }
-  const int ctas = PairSmem<D>::kPerSm * kNumSMs, chunk = chunk_of(n_seg, p.H, ctas);
+  const int ctas = PairSmem<D>::kPerSm * kNumSMs / p.H * p.H, chunk = chunk_of(n_seg, p.H, ctas);
   const long long items = (long long)((n_seg + chunk - 1) / chunk) * p.H;
   launch_pdl(kern, (int)(items < ctas ? items : ctas), kThreads, PairSmem<D>::kBytes + 2 * rel.view.pitch * 4, st, tm_qkv, tm_do, tm_o, lse, delta,
              seg, n_seg, chunk, p.capacity, p.C, p.H, softmax_scale_of(p), (__nv_bfloat16*)dqkv, rel, d_status);
@@ -794,9 +792,9 @@ int launch(const spa_params& p, const void* qkv, const void* ao, const float* ls
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTwoPerSm); });
   if (ea != cudaSuccess) { set_cuda_error(ea, "rel_bwd_short_kernel"); return SPA_ERR_CUDA; }
-  const int chunk = chunk_of(n_seg, p.H, 2 * kNumSMs);
+  const int ctas = 2 * kNumSMs / p.H * p.H, chunk = chunk_of(n_seg, p.H, ctas);
   const long long items = (long long)((n_seg + chunk - 1) / chunk) * p.H;
-  launch_pdl(kern, (int)(items < 2 * kNumSMs ? items : 2 * kNumSMs), kThreads, smem, st, tm_qkv, tm_do, tm_o, lse, delta, seg, n_seg, chunk,
+  launch_pdl(kern, (int)(items < ctas ? items : ctas), kThreads, smem, st, tm_qkv, tm_do, tm_o, lse, delta, seg, n_seg, chunk,
              least, p.capacity, p.C, p.H, softmax_scale_of(p), (__nv_bfloat16*)dqkv, rel, d_status);
   SPA_CUDA_CHECK_LAUNCH("rel_bwd_short_kernel");
   return SPA_OK;

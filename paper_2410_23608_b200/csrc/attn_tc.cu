@@ -840,7 +840,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     }
   }
   if constexpr (kRel != kNoRel) {  // the item before is through with all this
-    if (kRel == kRelShared) {
+    if (kRel == kRelShared && first_item) {  // a grid that strides over the items is a multiple of H: they are all of one head
       const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
       for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<float4*>(smem_al + kTableBase)[i] = from[i];
     }
@@ -1285,10 +1285,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     if constexpr (kRel != kNoRel) {
       if (kDQ && rel.shared_bins) {  // the item's bins to the head's sums
         const int shift = range[0];
-        for (int i = tid; i < rel.view.entries; i += kBwdThreads) {
-          const int v = reinterpret_cast<int*>(bins)[i];
-          if (v != 0) rel_add(rel.grad, h, i, rel_shifted(v, shift));
-        }
+        rel_flush<kBwdThreads>(rel, reinterpret_cast<const int*>(bins), h, shift, tid);
       }
       if (again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
     }
@@ -1432,7 +1429,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     ptx::tma_load_2d(x1_s, &tm_qkv, bar_x, x1_col, r0);
     ptx::tma_load_2d(x2_s, &tm_qkv, bar_x, 2 * C + h * D, r0);           // V
   }
-  if constexpr (kRel == kRelShared) {  // the item before is through with it
+  if (kRel == kRelShared && first_item) {  // see the dQ pass
     const float4* from = reinterpret_cast<const float4*>(rel.view.bias + (long long)h * rel.view.pitch);
     for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<float4*>(smem_al + kTableBase)[i] = from[i];
   }
@@ -2093,7 +2090,7 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   const bool even_items = (long long)p.capacity <= 256ll * (n_seg > 0 ? n_seg : 1);
   // (Behind the one-pass kernels of a problem with a bias few items are left, often none: a CTA per item cost 12 us of 95 for nothing.)
   const bool loop = (even_items && items >= 3ll * 2 * kNumSMs) || (kRel != kNoRel && long_only && items >= 2ll * kNumSMs);
-  const int grid = (int)(loop ? 2 * kNumSMs : items);
+  const int grid = (int)(!loop ? items : kRel == kNoRel ? 2 * kNumSMs : 2 * kNumSMs / p.H * p.H);
   auto kq = loop ? attn_bwd_tc_kernel<D, true, true, kRel> : attn_bwd_tc_kernel<D, true, false, kRel>;
   auto kkv = loop ? KV::template kernel<true>() : KV::template kernel<false>();
   const float scale = softmax_scale_of(p);
