@@ -216,10 +216,11 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
           if (need) {
             const uint64_t scale2 = ptx::pair(scale_log2e, scale_log2e), lse2 = ptx::pair(-my_lse, -my_lse), D2 = ptx::pair(-my_D, -my_D);
             const uint32_t pos_at = pos_s + 4 * col0;
+            RelKeys<> keys(pos_at);
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
               int k[4];
-              ptx::lds_4s32(pos_at + 4 * j, k);
+              keys.next(j, 32, k);
 #pragma unroll
               for (int u = 0; u < 4; u += 2) {
                 const float b0 = ptx::lds_f32(table_s + bias_at + k[u]), b1 = ptx::lds_f32(table_s + bias_at + k[u + 1]);
@@ -246,10 +247,11 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
               ptx::unpair(ptx::mul2(d, bin2), rp[j], rp[j + 1]);
             }
             // the table's gradient: a pair's bin is where its bias came from
+            RelKeys<> again(pos_at);
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
               int k[4];
-              ptx::lds_4s32(pos_at + 4 * j, k);
+              again.next(j, 32, k);
 #pragma unroll
               for (int u = 0; u < 4; ++u) ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rp[j + u])));
             }
@@ -593,10 +595,11 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
         if (valid && c0 < n) {
           const uint64_t scale2 = ptx::pair(scale_log2e, scale_log2e), lse2 = ptx::pair(-my_lse, -my_lse), D2 = ptx::pair(-my_D, -my_D);
           const uint32_t pos_at = pos_s + 4 * (64 * which + c0);
+          RelKeys<> keys(pos_at);
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
             int k[4];
-            ptx::lds_4s32(pos_at + 4 * j, k);
+            keys.next(j, 16, k);
 #pragma unroll
             for (int u = 0; u < 4; u += 2) {
               const float b0 = ptx::lds_f32(table_s + bias_at + k[u]), b1 = ptx::lds_f32(table_s + bias_at + k[u + 1]);
@@ -623,10 +626,11 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
             ptx::unpair(ptx::mul2(d, bin2), rp[j], rp[j + 1]);
           }
           // the table's gradient: a pair's bin is where its bias came from
+          RelKeys<> again(pos_at);
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
             int k[4];
-            ptx::lds_4s32(pos_at + 4 * j, k);
+            again.next(j, 16, k);
 #pragma unroll
             for (int u = 0; u < 4; ++u) ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rp[j + u])));
           }

@@ -510,15 +510,19 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
           if constexpr (kRel != kNoRel) {
             if (need[c]) {
               const uint32_t at = pos_q + (g & 1) * kKV * 4 + 4 * (col0 + c * 32);
+              RelKeys<> keys(at);
 #pragma unroll
               for (int j = 0; j < 32; j += 4) {
                 int k[4];
-                ptx::lds_4s32(at + 4 * j, k);
+                keys.next(j, 32, k);
+                float b[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                  const float b = kRel == kRelShared ? ptx::lds_f32(bias_at + k[u])
-                                                     : *reinterpret_cast<const float*>(bias_g + (bias_at + k[u]));
-                  s[c * 32 + j + u] = __float_as_uint(fmaf(__uint_as_float(s[c * 32 + j + u]), scale_log2e, b));
+                for (int u = 0; u < 4; ++u)
+                  b[u] = kRel == kRelShared ? ptx::lds_f32(bias_at + k[u]) : *reinterpret_cast<const float*>(bias_g + (bias_at + k[u]));
+#pragma unroll
+                for (int u = 0; u < 4; u += 2) {
+                  uint32_t* v = s + c * 32 + j + u;
+                  ptx::unpair(ptx::fma2(ptx::pair(v[0], v[1]), ptx::pair(scale_log2e, scale_log2e), ptx::pair(b[u], b[u + 1])), v[0], v[1]);
                 }
               }
             }
@@ -565,11 +569,20 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
           if (need[c]) {
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              const float s0 = __uint_as_float(s[c * 32 + j]), s1 = __uint_as_float(s[c * 32 + j + 1]);
-              const float p0 = ptx::ex2_approx(kRel != kNoRel ? s0 - m_use : fmaf(s0, scale_log2e, -m_use));  // -inf -> 0
-              const float p1 = ptx::ex2_approx(kRel != kNoRel ? s1 - m_use : fmaf(s1, scale_log2e, -m_use));
-              rs0 += p0;
-              rs1 += p1;
+              float s0 = __uint_as_float(s[c * 32 + j]), s1 = __uint_as_float(s[c * 32 + j + 1]);
+              if constexpr (kRel != kNoRel) {
+                ptx::unpair(ptx::add2(ptx::pair(s0, s1), ptx::pair(-m_use, -m_use)), s0, s1);
+              } else {
+                s0 = fmaf(s0, scale_log2e, -m_use);
+                s1 = fmaf(s1, scale_log2e, -m_use);
+              }
+              const float p0 = ptx::ex2_approx(s0), p1 = ptx::ex2_approx(s1);  // -inf -> 0
+              if constexpr (kRel != kNoRel) {
+                ptx::unpair(ptx::add2(ptx::pair(rs0, rs1), ptx::pair(p0, p1)), rs0, rs1);
+              } else {
+                rs0 += p0;
+                rs1 += p1;
+              }
               __nv_bfloat162 b = __floats2bfloat162_rn(p0, p1);  // low half = even key
               pk[c * 16 + (j >> 1)] = *reinterpret_cast<uint32_t*>(&b);
             }
@@ -1145,16 +1158,19 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
         const uint32_t pos_at = pos_s + ((t % 3) * kBwdY + col0) * 4;
         if constexpr (kRel != kNoRel) {  // S in units of log 2, with its bias
           const char* table = reinterpret_cast<const char*>(rel.view.bias + (long long)h * rel.view.pitch);
+          RelKeys<!kDQ> keys(pos_at);
 #pragma unroll
           for (int j = 0; j < kPc; j += 4) {
             int k[4];
-            ptx::lds_4s32(pos_at + 4 * j, k);
+            keys.next(j, kPc, k);
+            float b[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float b = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u])
-                                                 : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
-              rs[j + u] = __float_as_uint(fmaf(__uint_as_float(rs[j + u]), scale_log2e, b));
-            }
+            for (int u = 0; u < 4; ++u)
+              b[u] = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u]) : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
+#pragma unroll
+            for (int u = 0; u < 4; u += 2)
+              ptx::unpair(ptx::fma2(ptx::pair(rs[j + u], rs[j + u + 1]), ptx::pair(scale_log2e, scale_log2e), ptx::pair(b[u], b[u + 1])),
+                          rs[j + u], rs[j + u + 1]);
           }
         }
         if (!(yc0 >= mine.lo && yc0 + kPc <= mine.hi)) {
@@ -1179,36 +1195,56 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
 #pragma unroll
           for (int j = 0; j < kPc; j += 2) {
             float d0, d1;
-            ptx::unpair(ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1])), d0, d1);
+            const uint64_t d = ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1]));
+            ptx::unpair(d, d0, d1);
             pk_ds[j >> 1] = ptx::bf16_pair(d0, d1);
-            if (kRel != kNoRel) { rs[j] = __float_as_uint(d0); rs[j + 1] = __float_as_uint(d1); }
+            if (kRel != kNoRel) ptx::unpair(ptx::mul2(d, ptx::pair(bin_scale, bin_scale)), rs[j], rs[j + 1]);
           }
           if constexpr (kRel != kNoRel) {  // the table's gradient: a pair's bin is where its bias came from
+            RelKeys<!kDQ> keys(pos_at);
 #pragma unroll
             for (int j = 0; j < kPc; j += 4) {
               int k[4];
-              ptx::lds_4s32(pos_at + 4 * j, k);
+              keys.next(j, kPc, k);
               if (rel.shared_bins) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                  ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rs[j + u]) * bin_scale));
+                  ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rs[j + u])));
               } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                  rel_add(rel.grad, h, (int)(bias_at + k[u]) >> 2, __float2ll_rn(__uint_as_float(rs[j + u]) * bin_scale));
+                  rel_add(rel.grad, h, (int)(bias_at + k[u]) >> 2, __float2ll_rn(__uint_as_float(rs[j + u])));
               }
             }
           }
         } else {
           const float* sl = stat_lse + (t % 3) * kBwdY + col0;
           const float* sd = stat_D + (t % 3) * kBwdY + col0;
+          if constexpr (kRel != kNoRel) {
+            const uint32_t sl_s = smem_base + kStatBase + ((t % 3) * kBwdY + col0) * 4, sd_s = sl_s + 3 * kBwdY * 4;
+#pragma unroll
+            for (int j = 0; j < kPc; j += 4) {
+              uint64_t l2[2], d2[2];
+              ptx::lds_pairs(sl_s + 4 * j, l2[0], l2[1]);
+              ptx::lds_pairs(sd_s + 4 * j, d2[0], d2[1]);
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int i = j + 2 * u;
+                float e0, e1, d0, d1;
+                ptx::unpair(ptx::add2(ptx::pair(rs[i], rs[i + 1]), l2[u]), e0, e1);
+                const float p0 = ptx::ex2_approx(e0), p1 = ptx::ex2_approx(e1);
+                ptx::unpair(ptx::mul2(ptx::pair(p0, p1), ptx::add2(ptx::pair(rp[i], rp[i + 1]), d2[u])), d0, d1);
+                pk_ds[i >> 1] = ptx::bf16_pair(d0, d1);
+                pk_p[i >> 1] = ptx::bf16_pair(p0, p1);
+              }
+            }
+          } else
 #pragma unroll
           for (int j = 0; j < kPc; j += 2) {
             float pv[2], dsv[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              pv[u] = ptx::ex2_approx(kRel != kNoRel ? __uint_as_float(rs[j + u]) + sl[j + u]
-                                                     : fmaf(__uint_as_float(rs[j + u]), scale_log2e, sl[j + u]));
+              pv[u] = ptx::ex2_approx(fmaf(__uint_as_float(rs[j + u]), scale_log2e, sl[j + u]));
               dsv[u] = pv[u] * (__uint_as_float(rp[j + u]) + sd[j + u]);
             }
             pk_ds[j >> 1] = ptx::bf16_pair(dsv[0], dsv[1]);
@@ -1662,16 +1698,19 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
         if constexpr (kRel != kNoRel) {  // S in units of log 2, with its bias
           const char* table = reinterpret_cast<const char*>(rel.view.bias + (long long)h * rel.view.pitch);
           const uint32_t pos_at = pos_s + ((t % 3) * kBwdY + col0) * 4;
+          RelKeys<> keys(pos_at);
 #pragma unroll
           for (int j = 0; j < kPc; j += 4) {
             int k[4];
-            ptx::lds_4s32(pos_at + 4 * j, k);
+            keys.next(j, kPc, k);
+            float b[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float b = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u])
-                                                 : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
-              rs[j + u] = __float_as_uint(fmaf(__uint_as_float(rs[j + u]), scale_log2e, b));
-            }
+            for (int u = 0; u < 4; ++u)
+              b[u] = kRel == kRelShared ? ptx::lds_f32(table_s + bias_at + k[u]) : *reinterpret_cast<const float*>(table + (bias_at + k[u]));
+#pragma unroll
+            for (int u = 0; u < 4; u += 2)
+              ptx::unpair(ptx::fma2(ptx::pair(rs[j + u], rs[j + u + 1]), ptx::pair(scale_log2e, scale_log2e), ptx::pair(b[u], b[u + 1])),
+                          rs[j + u], rs[j + u + 1]);
           }
         }
         if (partial) {
