@@ -412,6 +412,8 @@ _GATE_KINDS = {"none": SPA_GATE_NONE, "score": SPA_GATE_SCORE, "image": SPA_GATE
 
 def sandwich(kind="layer", gate_kind="none", gate=None, scale=None, g_post=None, b_post=None, g_pre=None, b_pre=None, eps=1e-5) -> SpaSandwich:
     """A spa_sandwich from device tensors (which it keeps) and the names of its kinds ("layer", "rms"; "none", "score", "image", "token")."""
+    if gate_kind in ("score", SPA_GATE_SCORE) and (gate is None or gate.dtype != torch.float32):
+        raise ValueError("gate: the scores, float32 [B * N]")
     tensors = (gate, scale, g_post, b_post, g_pre, b_pre)
     s = SpaSandwich(_NORM_KINDS.get(kind, kind), _GATE_KINDS.get(gate_kind, gate_kind), float(eps), *(_ptr(t) for t in tensors))
     s.tensors = tensors

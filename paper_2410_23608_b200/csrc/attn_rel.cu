@@ -193,8 +193,8 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
     if ((unsigned)t < (unsigned)tokens && ld_dep(owner + t) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
   }
   if constexpr (kRedo) {
-    const int n = ld_dep(reinterpret_cast<const int32_t*>(g.redo));
-    for (int i = blockIdx.x * 8 + warp; i < n; i += gridDim.x * 8) redo_row(r, seg, n_seg, capacity, Np, g.redo[1 + i]);
+    const uint32_t noted = (uint32_t)ld_dep(reinterpret_cast<const int32_t*>(g.redo)), n = noted < g.most_redo ? noted : g.most_redo;
+    for (uint32_t i = blockIdx.x * 8 + warp; i < n; i += gridDim.x * 8) redo_row(r, seg, n_seg, capacity, Np, g.redo[1 + i]);
   }
 }
 
@@ -218,7 +218,7 @@ Layout layout(const spa_params& p, const spa_rel_bias& r) {
   l.bound = take((size_t)kRelBlocks * p.H * 8);
   l.bad = take((size_t)p.H * 4);
   l.owner = take((size_t)p.B * p.N * 4);
-  if (use_tc(p)) {
+  if (p.dtype == SPA_BF16) {  // whatever kernels take it
     l.delta = take((size_t)p.H * p.capacity * 4);
     l.redo = take(((size_t)4 * p.H * p.capacity + 1) * 4);
   } else {
@@ -309,11 +309,13 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   g.redo = (uint32_t*)(ws + l.redo);
   g.n_buckets = r.n_buckets;
   g.H = p.H;
+  g.most_redo = 4u * p.H * p.capacity;
   rc = tc ? launch_attention_rel_bwd_tc(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, (float*)(ws + l.delta), d_status, st)
           : launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);
   if (rc != SPA_OK) return rc;
   const long long work = (long long)r.n_buckets * p.H > p.capacity ? (long long)r.n_buckets * p.H : p.capacity;
-  const int grid = (int)((work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
+  // behind the tensor-core kernels a CTA per SM, should there be rows to form again
+  const int grid = (int)(!tc && (work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
   const Redo redo{view(l, ws), (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, lse, (const float*)(ws + l.delta), (__nv_bfloat16*)dqkv,
                p.C, p.C / p.H, softmax_scale_of(p)};
   launch_pdl(tc ? rel_finish_kernel<true> : rel_finish_kernel<false>, grid, 256, (size_t)p.H * sizeof(float), st, g, redo, seg, n_seg, p.capacity,

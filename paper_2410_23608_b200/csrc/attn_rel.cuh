@@ -40,12 +40,14 @@ struct RelGrad {
   int32_t* bad;             // [H] a row's statistics are not finite
   uint32_t* redo;           // [1 + 4 H capacity] how many, and which parts of rows are to be formed again
   int n_buckets, H;
+  uint32_t most_redo;       // 4 H capacity
 };
 
 // A zero weight times an infinity or NaN of another segment in the same tile is NaN.  Halves of rows of dQ (keys = false) or of dK
 // and dV that are not finite are noted down, and formed again behind the attention from their own segment's rows alone.
 __device__ __forceinline__ void rel_redo(const RelGrad& g, bool keys, int half, int h, int row) {
-  g.redo[1 + atomicAdd(g.redo, 1u)] = (uint32_t)row | (uint32_t)h << 20 | (keys ? 1u : 0u) << 28 | (uint32_t)half << 29;
+  const uint32_t at = atomicAdd(g.redo, 1u);
+  if (at < g.most_redo) g.redo[1 + at] = (uint32_t)row | (uint32_t)h << 20 | (keys ? 1u : 0u) << 28 | (uint32_t)half << 29;
 }
 
 // Bits of the head's bound.  A bin has at most one pair per query, 2^20 in all, and the bound is taken up to a power of two.

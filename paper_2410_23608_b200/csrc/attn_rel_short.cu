@@ -95,7 +95,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
     const int s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
     if (tid <= count) {
       const int o = ld_dep(seg + s0 + tid);
-      seg_s[tid] = o < Np ? o : Np;
+      seg_s[tid] = o < 0 ? 0 : (o < Np ? o : Np);
     }
     __syncthreads();
     int first = 0;
@@ -467,7 +467,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
     const int s0 = item / H * chunk, count = n_seg - s0 < chunk ? n_seg - s0 : chunk;
     if (tid <= count) {
       const int o = ld_dep(seg + s0 + tid);
-      seg_s[tid] = o < Np ? o : Np;
+      seg_s[tid] = o < 0 ? 0 : (o < Np ? o : Np);
     }
     __syncthreads();
     auto length = [&](int s) { return seg_s[s + 1] - seg_s[s]; };

@@ -144,8 +144,9 @@ __device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat
 template <int D, int kRel>
 __global__ void __launch_bounds__(kFwdThreads, 2)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, int n_seg, int capacity,
-                   int C, int H, float scale_log2e, const RelView rel, const __nv_bfloat16* qkv, __nv_bfloat16* __restrict__ ao,
-                   float* __restrict__ lse, float* __restrict__ peak, unsigned* counter, bool even_items, int32_t* d_status) {
+                   int C, int H, float scale_log2e, __nv_bfloat16* __restrict__ ao, float* __restrict__ lse,
+                   unsigned* counter, bool even_items, int32_t* d_status, const RelView rel, const __nv_bfloat16* qkv,
+                   float* __restrict__ peak) {
   using HT = HeadTile<D>;
   using SM = FwdSmem<D, kRel>;
   constexpr int kTile = HT::kTileBytes;
@@ -2173,8 +2174,8 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
   // 400 rows (and cost 1 us in front of short items), and 8 to 12 % from 576 rows on.
   const bool even_items = (long long)p.capacity <= 512ll * (n_seg > 0 ? n_seg : 1);
   launch_pdl(kern, grid, kFwdThreads, smem, st, tm, seg, n_seg, p.capacity, p.C, p.H,
-             softmax_scale_of(p) * 1.4426950408889634f, rel, (const __nv_bfloat16*)qkv, (__nv_bfloat16*)ao, lse, peak,
-             kRel == kNoRel && items > grid ? item_counter(ao) : nullptr, even_items, d_status);
+             softmax_scale_of(p) * 1.4426950408889634f, (__nv_bfloat16*)ao, lse, kRel == kNoRel && items > grid ? item_counter(ao) : nullptr,
+             even_items, d_status, rel, (const __nv_bfloat16*)qkv, peak);
   SPA_CUDA_CHECK_LAUNCH("attn_fwd_tc_kernel");
   return SPA_OK;
 }
