@@ -223,7 +223,7 @@ int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, c
 /* Gradient of spa_packed_attention_rel_fwd: dqkv as spa_packed_attention_bwd, and
  *   dtable[b][h] = sum of dS_ij over all pairs of all segments whose bucket is b     (float[n_buckets][H] out).
  * Bitwise reproducible: dS is summed in integers, as multiples of a power of two that is chosen by a bound on its size; each dS
- * is rounded by at most 2^-23 of the largest that its 128 query rows can have (fp32 problems: 2^-40 of its head's).  peak (of the
+ * is rounded by at most 2^-30 of the largest that its 128 query rows can have (fp32 problems: 2^-42 of its head's).  peak (of the
  * same forward call) makes that bound tight; without it (NULL) every probability counts as one that may be 1.  Where a value of V, K or
  * d_attn_out, or a row's lse or D, is not finite, the whole head's column of dtable may be NaN.  dqkv has infinities and NaN of a segment in
  * that segment's rows only (rows whose tile they reach are formed again: such a call is slower).  SPA_FLAG_ONE_PASS_BWD has no effect. */

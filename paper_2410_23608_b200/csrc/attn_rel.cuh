@@ -51,7 +51,7 @@ __device__ __forceinline__ void rel_redo(const RelGrad& g, bool keys, int half, 
 }
 
 // Bits of the head's bound.  A bin has at most one pair per query, 2^20 in all, and the bound is taken up to a power of two.
-constexpr int kRelBits = 40;
+constexpr int kRelBits = 42;
 
 // Exponent e of a bound b < 2^e; zero and values too small for the scale's exponent count as the smallest.
 __device__ __forceinline__ int rel_exponent(float b) {
@@ -100,12 +100,19 @@ struct RelBwd {
   RelGrad grad;
   bool shared_bins;
 };
-// The scale of an item's bins.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
-// with |dS| below 2^kRelItemBits in units of the scale a sum stays below 2^30.
-constexpr int kRelItemBits = 23;
+// The bins of an item are two words: a pair adds the low ten bits of its dS, a number below 2^kRelItemBits in units of the scale, to one and
+// the others to the other.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
+// neither overflows.  (One word holds 23 bits of a pair, and the bound is a thousand times what a pair has on average: the gradient of
+// 32 images of 24 x 24 tokens was off by 3.6e-5.)
+constexpr int kRelItemBits = 30, kRelLow = 10;
+__device__ __forceinline__ void rel_bin(uint32_t at, uint32_t pitch_bytes, float scaled) {
+  const int v = __float2int_rn(scaled);
+  ptx::red_add_s32(at, v & ((1 << kRelLow) - 1));
+  ptx::red_add_s32(at + pitch_bytes, v >> kRelLow);
+}
 // A sum in units of an item's scale as one in units of the head's
-__device__ __forceinline__ long long rel_shifted(int v, int shift) {
-  return shift >= 0 ? (long long)v << shift : (long long)v >> (shift > -63 ? -shift : 63);
+__device__ __forceinline__ long long rel_shifted(long long v, int shift) {
+  return shift >= 0 ? v << shift : v >> (shift > -63 ? -shift : 63);
 }
 
 // Positions of a tile's columns from shared memory, four at a time, and where registers allow (kAhead) a step before they are used: the
@@ -132,11 +139,12 @@ template <bool kAhead = true> struct RelKeys {
 template <int kThreads>
 __device__ __forceinline__ void rel_flush(const RelBwd& rel, const int* bins, int h, int shift, int tid) {
   for (int i = tid; i < rel.view.entries; i += 4 * kThreads) {
-    int v[4], b[4];
+    long long v[4];
+    int b[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int at = i + u * kThreads;
-      v[u] = at < rel.view.entries ? bins[at] : 0;
+      v[u] = at < rel.view.entries ? ((long long)bins[rel.view.pitch + at] << kRelLow) + bins[at] : 0;
       b[u] = v[u] != 0 ? rel.grad.bucket[at] : -1;
     }
 #pragma unroll

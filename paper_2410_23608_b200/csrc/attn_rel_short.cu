@@ -31,7 +31,7 @@ template <int D> struct Smem {
   static constexpr int kBar = kDS + kOp;           // barriers, TMEM slot, the tile's bound
   static constexpr int kSeg = kBar + 64;           // offsets of the CTA's segments
   static constexpr int kPos = kSeg + 192;          // the tile's key positions
-  static constexpr int kTable = kPos + 128 * 4;    // the head's table, and behind it the bins
+  static constexpr int kTable = kPos + 128 * 4;    // the head's table, and behind it the bins, two words each
   static constexpr int kBytes = kTable + 1024;     // and the alignment of the base
 };
 
@@ -117,7 +117,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
         ptx::tma_load_2d(do_s, &tm_do, bar_ld, h * D, lo);
         ptx::tma_load_2d(smem_base + SM::kO, &tm_o, bar_ld, h * D, lo);
       }
-      for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = tid; i < rel.view.pitch / 2; i += kThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
       const int row = lo + rl;
       const bool valid = rl < n;
       const int own_pos = rel.view.pos[row];
@@ -253,7 +253,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
               int k[4];
               again.next(j, 32, k);
 #pragma unroll
-              for (int u = 0; u < 4; ++u) ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rp[j + u])));
+              for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rp[j + u]));
             }
           }
           __syncwarp();
@@ -495,7 +495,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
           ptx::tma_load_2d(smem_base + o_off(s), &tm_o, bar_ld, h * D, lo);
         }
       }
-      for (int i = tid; i < rel.view.pitch / 4; i += kThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = tid; i < rel.view.pitch / 2; i += kThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
       const int lo = which == 0 ? lo_a : lo_b, n = which == 0 ? n_a : n_b, row = lo + rr;
       const bool valid = rr < n;
       const int own_pos = rel.view.pos[row];
@@ -632,7 +632,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
             int k[4];
             again.next(j, 16, k);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rp[j + u])));
+            for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rp[j + u]));
           }
         }
         __syncwarp();
@@ -777,7 +777,7 @@ int launch_pair(const spa_params& p, const void* qkv, const void* ao, const floa
   if (ea != cudaSuccess) { set_cuda_error(ea, "rel_bwd_pair_kernel"); return SPA_ERR_CUDA; }
   const int ctas = PairSmem<D>::kPerSm * kNumSMs / p.H * p.H, chunk = chunk_of(n_seg, p.H, ctas);
   const long long items = (long long)((n_seg + chunk - 1) / chunk) * p.H;
-  launch_pdl(kern, (int)(items < ctas ? items : ctas), kThreads, PairSmem<D>::kBytes + 2 * rel.view.pitch * 4, st, tm_qkv, tm_do, tm_o, lse, delta,
+  launch_pdl(kern, (int)(items < ctas ? items : ctas), kThreads, PairSmem<D>::kBytes + 3 * rel.view.pitch * 4, st, tm_qkv, tm_do, tm_o, lse, delta,
              seg, n_seg, chunk, p.capacity, p.C, p.H, softmax_scale_of(p), (__nv_bfloat16*)dqkv, rel, d_status);
   SPA_CUDA_CHECK_LAUNCH("rel_bwd_pair_kernel");
   return SPA_OK;
@@ -792,7 +792,7 @@ int launch(const spa_params& p, const void* qkv, const void* ao, const float* ls
       !make_tmap_bf16_2d(&tm_o, ao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, 128, D * 2))
     return SPA_ERR_UNSUPPORTED;
   auto kern = rel_bwd_short_kernel<D>;
-  const int smem = Smem<D>::kBytes + 2 * rel.view.pitch * 4;
+  const int smem = Smem<D>::kBytes + 3 * rel.view.pitch * 4;
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTwoPerSm); });
   if (ea != cudaSuccess) { set_cuda_error(ea, "rel_bwd_short_kernel"); return SPA_ERR_CUDA; }
@@ -808,7 +808,7 @@ int launch(const spa_params& p, const void* qkv, const void* ao, const float* ls
 
 bool attention_rel_bwd_short_applies(const spa_params& p, int n_seg, const RelView& view) {
   const int base = p.C / p.H == 64 ? Smem<64>::kBytes : Smem<32>::kBytes;
-  return n_seg >= 1 && (long long)p.capacity <= 256ll * n_seg && base + 2 * view.pitch * 4 <= kTwoPerSm;
+  return n_seg >= 1 && (long long)p.capacity <= 256ll * n_seg && base + 3 * view.pitch * 4 <= kTwoPerSm;
 }
 
 int launch_attention_rel_bwd_short(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
@@ -817,8 +817,8 @@ int launch_attention_rel_bwd_short(const spa_params& p, const void* qkv, const v
   // two to a tile where most segments are of at most 64 rows and the tables fit; a segment is of one image, which may rule out longer ones
   const bool d64 = p.C / p.H == 64;
   const bool pairs = (p.N <= kPairMax || (n_seg >= 2 * p.B && (long long)p.capacity <= (long long)kPairMax * n_seg)) &&
-                     (d64 ? PairSmem<64>::kBytes <= PairSmem<64>::kMost - 2 * rel.view.pitch * 4
-                          : PairSmem<32>::kBytes <= PairSmem<32>::kMost - 2 * rel.view.pitch * 4);
+                     (d64 ? PairSmem<64>::kBytes <= PairSmem<64>::kMost - 3 * rel.view.pitch * 4
+                          : PairSmem<32>::kBytes <= PairSmem<32>::kMost - 3 * rel.view.pitch * 4);
   if (pairs) {
     const int rc = d64 ? launch_pair<64>(p, qkv, ao, lse, dao, seg, n_seg, rel, dqkv, delta, d_status, st)
                        : launch_pair<32>(p, qkv, ao, lse, dao, seg, n_seg, rel, dqkv, delta, d_status, st);

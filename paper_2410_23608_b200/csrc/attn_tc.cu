@@ -860,7 +860,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     }
     if (kDQ) {
       if (rel.shared_bins)
-        for (int i = tid; i < rel.view.pitch / 4; i += kBwdThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = tid; i < rel.view.pitch / 2; i += kBwdThreads) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
       if (tid == 0) *item_bound = 0u;
     }
   }
@@ -1210,7 +1210,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
               if (rel.shared_bins) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                  ptx::red_add_s32(bins_s + bias_at + k[u], __float2int_rn(__uint_as_float(rs[j + u])));
+                  rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rs[j + u]));
               } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -2100,11 +2100,11 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
     return SPA_ERR_UNSUPPORTED;
   using KV = kv_pass<D, kRel>;
   const int table = kRel == kNoRel ? 0 : rel.view.pitch * 4;
-  int dq_smem = bwd_smem_bytes<D, true, kRel>() + (kRel == kRelShared ? 2 * table : 0);
+  int dq_smem = bwd_smem_bytes<D, true, kRel>() + (kRel == kRelShared ? 3 * table : 0);
   if (kRel == kRelShared) rel.shared_bins = true;
   if (kRel == kRelGlobal) {
-    rel.shared_bins = dq_smem + table <= kOnePerSm;
-    if (rel.shared_bins) dq_smem += table;
+    rel.shared_bins = dq_smem + 2 * table <= kOnePerSm;
+    if (rel.shared_bins) dq_smem += 2 * table;
   }
   const int kv_smem = KV::kSmem + (kRel == kRelShared ? table : 0);
   static DeviceOnce attr;
@@ -2221,11 +2221,11 @@ int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void
   }
 #define SPA_REL_BWD(D, REL) bwd_launch<D, REL>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, one_pass, d_status, st)
   if (p.C / p.H == 64) {
-    if (bwd_smem_bytes<64, true, kRelShared>() + 2 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
+    if (bwd_smem_bytes<64, true, kRelShared>() + 3 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
       return SPA_REL_BWD(64, kRelShared);
     return SPA_REL_BWD(64, kRelGlobal);
   }
-  if (bwd_smem_bytes<32, true, kRelShared>() + 2 * table <= kTwoPerSm && bwd_smem_bytes<32, false, kRelShared>() + table <= kTwoPerSm)
+  if (bwd_smem_bytes<32, true, kRelShared>() + 3 * table <= kTwoPerSm && bwd_smem_bytes<32, false, kRelShared>() + table <= kTwoPerSm)
     return SPA_REL_BWD(32, kRelShared);
   return SPA_REL_BWD(32, kRelGlobal);
 #undef SPA_REL_BWD

@@ -112,12 +112,12 @@ def check(run, flags=0, peak=True, seg=None, scale=None):
     assert np.all(np.abs(g[:Np] - b["dqkv"]) <= tol), np.max(np.abs(g[:Np] - b["dqkv"]) / tol)
     assert np.all(g[Np:] == Run.GUARD)
     # the integer bins: half a unit per pair, of a power of two up to twice the bound 2 max |dO| max |v| (times the largest
-    # probability, with peak): 2^-23 of the bound on tensor cores, 2^-40 otherwise
+    # probability, with peak): 2^-30 of the bound on tensor cores, 2^-42 otherwise
     half = 0.0
     if Np:
         v = pr["qkv"][:, 2 * C:].reshape(Np, H, d)
         bound = 2 * np.sqrt((v ** 2).sum(2).max()) * np.sqrt((pr["d_out"].reshape(Np, H, d) ** 2).sum(2).max())
-        half = bound * (2.0 ** -23 if tc else 2.0 ** -40)
+        half = bound * (2.0 ** -30 if tc else 2.0 ** -42)
     tol = b["dtable_tol"] + half * b["count"] + 2 * U * np.abs(b["dtable"]) + 1e-30
     g = host(run.dtable)
     assert np.all(np.abs(g - b["dtable"]) <= tol), np.max(np.abs(g - b["dtable"]) / tol)
