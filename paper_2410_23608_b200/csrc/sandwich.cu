@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
       float u[kU * R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if (kGate == SPA_GATE_SCORE) score[r] = sigmoid(score[r]);
+        if (kGate == SPA_GATE_SCORE) score[r] = has[r] ? sigmoid(score[r]) : 0.f;  // without a row it may be NaN, or was not copied
         const uint64_t rs = both(r1[r]), m = both(-m1[r] * r1[r]), w = both(score[r]);
         uint64_t u1 = 0ull, u2 = 0ull, u3 = 0ull;
 #pragma unroll

@@ -268,3 +268,24 @@ def test_empty_batch_clears_the_sums():
     L.spa_sandwich_norm_bwd(p, sw, t, t, t, t, None, t, t, t, dscale=grad, workspace=ws)
     torch.cuda.synchronize()
     assert bool((grad == 0).all()) and bool((t == 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [64, 768, 4096])
+@pytest.mark.parametrize("what", ["score", "z"])
+def test_values_that_are_not_finite_beside_the_selection(dtype, C, what):
+    """Tokens without a row have scores that are NaN, rows of z that no token names are NaN: nothing changes."""
+    pr = problem(dtype, 3, 45, C, "layer", "score", keep=0.5, seed=C)
+    clean = Run(pr)
+    clean.fwd(); clean.bwd()
+    run = Run(pr)
+    if what == "score":
+        run.gate[torch.from_numpy(pr["row"] < 0).cuda()] = float("nan")
+    else:
+        run.z[pr["z"].shape[0]:] = float("nan")
+    run.fwd(); run.bwd()
+    torch.cuda.synchronize()
+    for k in ("y", "n", "stats", "dx", "dz", "dgate"):
+        assert torch.equal(getattr(run, k), getattr(clean, k)), k
+    for k, g in run.grads.items():
+        assert torch.equal(g, clean.grads[k]), k
