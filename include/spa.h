@@ -201,8 +201,8 @@ int spa_packed_attention_bwd_static(const spa_params* p, const void* qkv, const 
  * (the idx of spa_select_pack; N must equal rows * cols).  (The backbone that the paper's blocks belong to, Sec. 3.1, has such
  * a bias in its attentions; the paper does not say how packed tokens are to have it.)
  *   bucket: int32[(2 rows - 1) * (2 cols - 1)], each in [0, n_buckets): a bucket for every offset, or few for many;
- *   table: T[n_buckets][H].  An entry of -inf masks its bucket; a row that is left without a key gives zeros, lse = -inf,
- *   peak = 0 and no gradient.
+ *   table: T[n_buckets][H].  An entry of -inf, or below -1e6, masks its bucket; a row that is left without a key gives zeros,
+ *   lse = -inf, peak = 0 and no gradient.
  * peak: float[H][capacity] out, the logarithm of the row's largest probability (max_j S_ij - lse_i), for the backward.
  * A segment must hold tokens of one image (images, or parts of them such as containers), and no token twice: the device records
  * SPA_ERR_INVALID_ARG in d_status where it does not, and for an idx or a bucket out of range (no access goes out of bounds; the

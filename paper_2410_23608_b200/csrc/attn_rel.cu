@@ -11,6 +11,9 @@ namespace spa {
 namespace {
 
 constexpr int kPrepThreads = 512;
+// Entries below this mask: beside any other they have no weight, and where a row has nothing else, its logarithm of the sum would have no bits
+// left for S (a type's lowest value times log2 e is not even finite).  Such rows are rows without a key.
+constexpr float kMasked = -1e6f;
 constexpr float kLog2e = 1.4426950408889634f;  // the tensor-core kernels take exponentials in base 2
 
 bool use_tc(const spa_params& p) { return !(p.flags & SPA_FLAG_SIMT_ONLY) && tc_attention_fwd_supported(p); }
@@ -48,8 +51,11 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
     const int b = o < a.entries ? a.bucket[o] : 0;
     const bool ok = (unsigned)b < (unsigned)a.n_buckets;
     if (!ok) record_status(d_status, SPA_ERR_INVALID_ARG);
-    for (int h = 0; h < a.H; ++h)
-      a.bias[(long long)h * a.pitch + o] = ok ? to_f32<T>(table[(long long)b * a.H + h]) * a.mul : 0.f;
+    for (int h = 0; h < a.H; ++h) {
+      float v = ok ? to_f32<T>(table[(long long)b * a.H + h]) : 0.f;
+      if (v < kMasked) v = -CUDART_INF_F;
+      a.bias[(long long)h * a.pitch + o] = v * a.mul;
+    }
   }
   for (int i = tid; i < a.capacity + 128; i += all) {
     int p = 0;

@@ -157,7 +157,7 @@ def test_masking_entries_and_rows_without_a_key(dtype, d, flags, mask):
 
 @pytest.mark.parametrize("dtype,d,flags", KINDS)
 def test_lowest_value_of_the_type_as_mask(dtype, d, flags):
-    """A table entry of the type's lowest finite value: no weight beside other keys, uniform weights where it is all there is."""
+    """A table entry of the type's lowest finite value: no weight beside other keys."""
     pr = problem(dtype, d, 1, 5, 5, (25, 12), seed=4)
     low = float(torch.finfo(torch.float32 if dtype == "f32" else torch.bfloat16).min)
     pr["table"][::3] = low
@@ -171,6 +171,18 @@ def test_lowest_value_of_the_type_as_mask(dtype, d, flags):
     assert np.isfinite(got).all() and torch.isfinite(run.dqkv).all()
     tol = (U * (d + 20) * 8 + (W if dtype == "bf16" else 0)) * f["mean_abs"] + (W if dtype == "bf16" else U) * np.abs(f["out"])
     assert np.all(np.abs(got - f["out"])[keep] <= 2 * tol[keep])
+
+
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("low", [-1e9, "lowest"])
+@pytest.mark.parametrize("grid,counts", [((9, 11), (99, 1, 40, 66)), ((14, 15), (210, 130))])
+def test_entries_that_mask_without_being_infinite(dtype, d, flags, low, grid, counts):
+    """What is below -1e6 masks as -inf does, where it is all that a row has, too: forward and backward as with -inf."""
+    pr = problem(dtype, d, 2, *grid, counts, seed=4, mask=0.99)
+    masked = np.isinf(pr["table"])
+    run = Run(pr, flags)
+    run.rel.tensors[1][torch.from_numpy(masked).cuda()] = torch.finfo(run.qkv.dtype).min if low == "lowest" else low
+    check(run, flags)
 
 
 @pytest.mark.parametrize("dtype,d,flags", KINDS)
