@@ -306,13 +306,13 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
         for (int d = 0; d < W; ++d) o[i][d] = fmaf(p, to_f32<T>(key[C + tx * W + d]), o[i][d]);
       }
     }
-    // biases of -inf may leave a row without a key: zeros
-    const float inv_l = kRel && l[i] == 0.f ? 0.f : 1.f / l[i];
+    const bool keyless = kRel && l[i] == 0.f;  // biases of -inf may leave a row without a key: zeros, whatever V is
+    const float inv_l = 1.f / l[i];
 #pragma unroll
-    for (int d = 0; d < W; ++d) o[i][d] *= inv_l;
+    for (int d = 0; d < W; ++d) o[i][d] = keyless ? 0.f : o[i][d] * inv_l;
     store_row<T, W>(ao + (long long)row * C + h * D + tx * W, o[i]);
     if (tx == 0) lse[(long long)h * capacity + row] = m[i] + logf(l[i]);
-    if (kRel && tx == 0) peak[(long long)h * capacity + row] = l[i] == 0.f ? 0.f : -logf(l[i]);
+    if (kRel && tx == 0) peak[(long long)h * capacity + row] = keyless ? 0.f : -logf(l[i]);
   }
 }
 

@@ -645,13 +645,17 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       ptx::named_barrier(1 + quarter, 64);
       const int rows = ptx::lds_s32(item_slot(it) + 68);
       const float l_row = xl[half * 128 + rl] + xl[(half ^ 1) * 128 + rl];
-      // biases of -inf may leave a row without a key: zeros
-      const float inv_l = kRel != kNoRel && l_row == 0.f ? 0.f : 1.f / l_row;
+      // biases of -inf may leave a row without a key: zeros, whatever V is
+      const bool keyless = kRel != kNoRel && l_row == 0.f;
+      const float inv_l = keyless ? 0.f : 1.f / l_row;
       bool again = false;
       if constexpr (kRel != kNoRel) {
         float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
+        for (int e = 0; e < kDh; ++e) {
+          if (keyless) r[e] = 0u;
+          sum += fabsf(__uint_as_float(r[e]));
+        }
         again = !(sum < CUDART_INF_F) && rl < rows;
       }
       uint4 o16[kDh / 8];
@@ -679,7 +683,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       if (half == 0 && rl < rows) {
         lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
         if (kRel != kNoRel)
-          peak[(long long)h * capacity + row] = l_row == 0.f ? 0.f : ((top - m) - log2f(l_row)) * 0.6931471805599453f;
+          peak[(long long)h * capacity + row] = keyless ? 0.f : ((top - m) - log2f(l_row)) * 0.6931471805599453f;
       }
       __syncwarp();
     }

@@ -186,6 +186,21 @@ def test_entries_that_mask_without_being_infinite(dtype, d, flags, low, grid, co
 
 
 @pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("own", [False, True])
+def test_rows_without_a_key_beside_infinities(dtype, d, flags, own):
+    """They are zeros and have no gradient, whatever V is, in their segment or in one that shares their tile."""
+    pr = problem(dtype, d, 1, 7, 9, (40, 30), seed=6)
+    pr["table"][:] = -np.inf
+    run = Run(pr, flags)
+    run.qkv[5 if own else 45, 2 * pr["C"] + 3] = float("inf")
+    run.fwd(); run.bwd()
+    torch.cuda.synchronize()
+    assert bool((run.out[:40] == 0).all()) and bool((run.lse[:, :40] == -float("inf")).all()) and bool((run.peak[:, :40] == 0).all())
+    if not own:
+        assert bool((run.dqkv[:40] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
 def test_large_logits_and_the_moving_maximum(dtype, d, flags):
     pr = problem(dtype, d, 2, 16, 20, (320, 250), seed=8, std=3.0)
     pr["table"] = round_to(40.0 * np.linspace(-1, 1, pr["table"].size).reshape(pr["table"].shape), dtype)
