@@ -224,9 +224,10 @@ int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, c
  *   dtable[b][h] = sum of dS_ij over all pairs of all segments whose bucket is b     (float[n_buckets][H] out).
  * Bitwise reproducible: dS is summed in integers, as multiples of a power of two that is chosen by a bound on its size; each dS
  * is rounded by at most 2^-30 of the largest that its 128 query rows can have (fp32 problems: 2^-42 of its head's).  peak (of the
- * same forward call) makes that bound tight; without it (NULL) every probability counts as one that may be 1.  Where a value of V, K or
- * d_attn_out, or a row's lse or D, is not finite, the whole head's column of dtable may be NaN.  dqkv has infinities and NaN of a segment in
- * that segment's rows only (rows whose tile they reach are formed again: such a call is slower).  SPA_FLAG_ONE_PASS_BWD has no effect. */
+ * same forward call) makes that bound tight; without it (NULL) every probability counts as one that may be 1.  No norm of a row of V
+ * or d_attn_out counts as less than 2^-63.  Where a value of V, K or d_attn_out, the square of a row's norm, or a row's lse or D is
+ * not finite, the whole head's column of dtable may be NaN.  dqkv has infinities and NaN of a segment in that segment's rows only
+ * (rows whose tile they reach are formed again: such a call is slower).  SPA_FLAG_ONE_PASS_BWD has no effect. */
 int spa_packed_attention_rel_bwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const void* attn_out, const float* lse,
                                  const float* peak, const void* d_attn_out, const int32_t* seg_offsets, int32_t n_seg,
                                  const int32_t* idx, void* dqkv, float* dtable, void* workspace, int32_t* d_status, void* stream);

@@ -60,10 +60,12 @@ __device__ __forceinline__ int rel_exponent(float b) {
 }
 __device__ __forceinline__ float rel_scale(int e) { return __uint_as_float((uint32_t)(127 + kRelBits - e) << 23); }
 
-// 2 max |dO| max |v| of a head, and max |v|, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.
+// 2 max |dO| max |v| of a head, and max |v|, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.  Squares that
+// underflow count as the smallest normal number: a bound may be too large, not too small.
+constexpr uint32_t kLeastSquare = 0x00800000u;
 __device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h, float& most_v) {
   const int lane = threadIdx.x & 31;
-  uint32_t v = 0, d = 0;
+  uint32_t v = kLeastSquare, d = kLeastSquare;
 #pragma unroll
   for (int i = 0; i < (kRelBlocks + 31) / 32; ++i) {
     if (lane + 32 * i < kRelBlocks) {
@@ -80,6 +82,11 @@ __device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h, float& 
 __device__ __forceinline__ float rel_head_bound(const RelGrad& g, int h) {
   float most_v;
   return rel_head_bound(g, h, most_v);
+}
+// The same of a row, from |dO|^2 and the logarithm of its largest probability, as a bit pattern
+__device__ __forceinline__ uint32_t rel_row_bound(float most_v, float square, float peak) {
+  const float d = square < __uint_as_float(kLeastSquare) ? __uint_as_float(kLeastSquare) : square;  // a NaN stays one
+  return __float_as_uint(2.f * most_v * sqrtf(d) * ptx::ex2_approx(peak * 1.4426950408889634f)) & 0x7fffffffu;
 }
 
 // A row whose logarithm of the sum (NaN, +inf) or D is not finite has dS that are not

@@ -160,8 +160,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
       }
       // a row without a key (lse = -inf, by its biases) has no weights
       my_lse = my_lse == -CUDART_INF_F ? CUDART_INF_F : my_lse * kLog2e;
-      const float bound = 2.f * head_v * sqrtf(row_norm) * ptx::ex2_approx(row_peak * kLog2e);
-      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(bound) & 0x7fffffffu);
+      const uint32_t most = __reduce_max_sync(0xffffffffu, valid ? rel_row_bound(head_v, row_norm, row_peak) : 0u);
       if (half == 0 && lane == 0) atomicMax(tile_bound, most);
       // lines behind the tile's rows are other segments' or unspecified memory: the products behind sum over the rows of Q, K and dO
       {
@@ -538,8 +537,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
         }
       }
       my_lse = my_lse == -CUDART_INF_F ? CUDART_INF_F : my_lse * kLog2e;  // a row without a key has no weights
-      const float bound = 2.f * head_v * sqrtf(row_norm) * ptx::ex2_approx(row_peak * kLog2e);
-      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(bound) & 0x7fffffffu);
+      const uint32_t most = __reduce_max_sync(0xffffffffu, valid ? rel_row_bound(head_v, row_norm, row_peak) : 0u);
       if (half == 0 && lane == 0) atomicMax(tile_bound, most);
       // lines behind the segments' rows are other segments', unspecified memory, or an earlier tile's
       for (int i = tid; i < (128 - n_a - n_b) * kChunks; i += kThreads) {

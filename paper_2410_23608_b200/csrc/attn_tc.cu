@@ -1116,8 +1116,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     if constexpr (kRel != kNoRel && kDQ) {
       if (half == 0 && mine.hi > mine.lo) rel_check_row(rel.grad, h, my_lse == CUDART_INF_F ? 0.f : my_lse, my_D);
       if (rel.shared_bins) {
-        const float b = 2.f * head_v * sqrtf(row_norm) * ptx::ex2_approx(row_peak * kLog2e);
-        const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(b) & 0x7fffffffu);
+        const uint32_t most = __reduce_max_sync(0xffffffffu, mine.hi > mine.lo ? rel_row_bound(head_v, row_norm, row_peak) : 0u);
         if (lane == 0) atomicMax(item_bound, most);
         ptx::named_barrier(1, kBwdMath);
         const int e = rel_exponent(__uint_as_float(*reinterpret_cast<volatile uint32_t*>(item_bound)));

@@ -201,6 +201,29 @@ def test_rows_without_a_key_beside_infinities(dtype, d, flags, own):
 
 
 @pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("v_std,d_std", [(1e-24, 1e12), (1e15, 1e-26)])
+def test_table_gradient_of_values_whose_squares_vanish(dtype, d, flags, v_std, d_std):
+    """The bound that the sums are scaled by is taken from squares: they may underflow, the bound may not."""
+    pr = problem(dtype, d, 2, 7, 9, (40, 63, 30), nb=6, seed=7)
+    C, H = pr["C"], pr["H"]
+    pr["qkv"][:, 2 * C:] = round_to(pr["qkv"][:, 2 * C:] * v_std, dtype)
+    pr["d_out"] = round_to(pr["d_out"] * d_std, dtype)
+    run = Run(pr, flags)
+    run.fwd(); run.bwd()
+    torch.cuda.synchronize()
+    args = (pr["cu"], pr["idx"], pr["rows"], pr["cols"], pr["bucket"], pr["table"], H)
+    lse = host(run.lse)[:, :run.Np]
+    s_err = (d + 7) * U * R.rel_fwd(pr["qkv"], *args)["s_abs"]
+    b = R.rel_bwd(pr["qkv"], host(run.out)[:run.Np], lse, pr["d_out"], *args, p_err=s_err + (8 + 3 * np.abs(lse).max()) * U, dot_err=(d + 2) * U)
+    # half a unit per pair, as elsewhere, of a bound for which neither norm is below 2^-63
+    most = lambda x: max(2.0 ** -63, np.sqrt((x.reshape(run.Np, H, d) ** 2).sum(2).max()))
+    half = 2 * most(pr["d_out"]) * most(pr["qkv"][:, 2 * C:]) * 2.0 ** -30
+    g = host(run.dtable)
+    tol = b["dtable_tol"] + half * b["count"] + 2 * U * np.abs(b["dtable"])
+    assert np.all(np.abs(g - b["dtable"]) <= tol), np.max(np.abs(g - b["dtable"]) / tol)
+
+
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
 def test_large_logits_and_the_moving_maximum(dtype, d, flags):
     pr = problem(dtype, d, 2, 16, 20, (320, 250), seed=8, std=3.0)
     pr["table"] = round_to(40.0 * np.linspace(-1, 1, pr["table"].size).reshape(pr["table"].shape), dtype)
