@@ -67,6 +67,9 @@ __device__ __forceinline__ void transpose_quads(uint4 (&c)[4], int lane) {
   swap(c[0], c[2], 2);
   swap(c[1], c[3], 2);
 }
+constexpr int kOnePerSm = 227 * 1024;
+// No more than a CTA per SM: it may take all of the SM's memory
+bool few_items(const spa_params& p) { return (long long)p.H * ((p.capacity + kQ - 1) / kQ) <= kNumSMs; }
 // Where the bias by relative position is read (attn_rel.cu): nowhere, in shared memory, in global memory
 enum RelTable { kNoRel = 0, kRelShared = 1, kRelGlobal = 2 };
 
@@ -2074,7 +2077,6 @@ attn_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_c
   }
 }
 
-constexpr int kOnePerSm = 227 * 1024;
 
 // Which kernel runs the dK / dV pass for head dimension D.
 template <int D, int kRel> struct kv_pass {
@@ -2088,9 +2090,9 @@ template <int kRel> struct kv_pass<64, kRel> {
   template <bool kLoop> static auto kernel() { return attn_bwd_kv_split_kernel<64, kLoop, kRel>; }
 };
 
-// kRel: rel is used, and the memory that the tables need is added to the kernels' own.  The bins of the dQ pass come first (kRelGlobal:
-// they may take a whole SM's memory), then the table.
-template <int D, int kRel>
+// kRel, kRelKV: rel is used by the dQ and by the dK / dV pass, and the memory that the tables need is added to the kernels' own.  The
+// bins of the dQ pass come first (kRelGlobal: they may take a whole SM's memory), then the table.
+template <int D, int kRel, int kRelKV = kRel>
 int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                const int32_t* seg, int n_seg, void* dqkv, void* workspace, RelBwd rel, bool long_only, int32_t* d_status,
                cudaStream_t st) {
@@ -2101,7 +2103,7 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
       !make_tmap_bf16_2d(&tm_do_y, dao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, kBwdY, D * 2) ||
       !make_tmap_bf16_2d(&tm_o, ao, (uint64_t)p.C, p.capacity, 2ull * p.C, D, 128, D * 2))
     return SPA_ERR_UNSUPPORTED;
-  using KV = kv_pass<D, kRel>;
+  using KV = kv_pass<D, kRelKV>;
   const int table = kRel == kNoRel ? 0 : rel.view.pitch * 4;
   int dq_smem = bwd_smem_bytes<D, true, kRel>() + (kRel == kRelShared ? 3 * table : 0);
   if (kRel == kRelShared) rel.shared_bins = true;
@@ -2109,12 +2111,12 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
     rel.shared_bins = dq_smem + 2 * table <= kOnePerSm;
     if (rel.shared_bins) dq_smem += 2 * table;
   }
-  const int kv_smem = KV::kSmem + (kRel == kRelShared ? table : 0);
+  const int kv_smem = KV::kSmem + (kRelKV == kRelShared ? table : 0);
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] {
     const auto smem_attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    constexpr int kDqMost = kRel == kRelGlobal ? kOnePerSm : kRel == kRelShared ? kTwoPerSm : bwd_smem_bytes<D, true>();
-    constexpr int kKvMost = kRel == kRelShared ? kTwoPerSm : KV::kSmem;
+    constexpr int kDqMost = kRel != kNoRel ? kOnePerSm : bwd_smem_bytes<D, true>();
+    constexpr int kKvMost = kRelKV == kRelShared ? kOnePerSm : KV::kSmem;
     cudaError_t e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, false, kRel>, smem_attr, kDqMost);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_bwd_tc_kernel<D, true, true, kRel>, smem_attr, kDqMost);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_bwd_short_kernel<D>, smem_attr, short_smem_bytes<D>());
@@ -2166,7 +2168,7 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
   const int smem = FwdSmem<D, kRel>::bytes(rel.pitch);
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] {
-    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRel == kRelShared ? kTwoPerSm : smem);
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRel == kRelShared ? kOnePerSm : smem);
   });
   if (ea != cudaSuccess) { set_cuda_error(ea, "attn_fwd_tc_kernel"); return SPA_ERR_CUDA; }
   // a persistent grid: two CTAs per SM (at most 94 KB of shared memory, 256 TMEM columns each), never more than work items
@@ -2186,7 +2188,7 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
 template <int D>
 int rel_fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
                    float* peak, int32_t* d_status, cudaStream_t st) {
-  if (FwdSmem<D, kRelShared>::bytes(rel.pitch) <= kTwoPerSm)
+  if (FwdSmem<D, kRelShared>::bytes(rel.pitch) <= (few_items(p) ? kOnePerSm : kTwoPerSm))
     return fwd_launch<D, kRelShared>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
   return fwd_launch<D, kRelGlobal>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
 }
@@ -2222,15 +2224,20 @@ int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void
     const int rc = launch_attention_rel_bwd_short(p, qkv, ao, lse, dao, seg, n_seg, rel, dqkv, delta, d_status, st);
     if (rc != SPA_OK || p.N <= kShortMax) return rc;  // a segment is of one image: there are no longer ones
   }
-#define SPA_REL_BWD(D, REL) bwd_launch<D, REL>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, one_pass, d_status, st)
-  if (p.C / p.H == 64) {
-    if (bwd_smem_bytes<64, true, kRelShared>() + 3 * table <= kTwoPerSm && split_smem_bytes<64, kRelShared>() + table <= kTwoPerSm)
-      return SPA_REL_BWD(64, kRelShared);
-    return SPA_REL_BWD(64, kRelGlobal);
-  }
-  if (bwd_smem_bytes<32, true, kRelShared>() + 3 * table <= kTwoPerSm && bwd_smem_bytes<32, false, kRelShared>() + table <= kTwoPerSm)
-    return SPA_REL_BWD(32, kRelShared);
-  return SPA_REL_BWD(32, kRelGlobal);
+  const bool few = few_items(p);
+  const int most = few ? kOnePerSm : kTwoPerSm;
+  const bool d64 = p.C / p.H == 64;
+  const int dq = d64 ? bwd_smem_bytes<64, true, kRelShared>() : bwd_smem_bytes<32, true, kRelShared>();
+  const int kv = d64 ? split_smem_bytes<64, kRelShared>() : bwd_smem_bytes<32, false, kRelShared>();
+  // the table in shared memory where that leaves as many CTAs on an SM as there would be without it
+  const bool dq_shared = dq + 3 * table <= (dq + 2 * table > kTwoPerSm ? kOnePerSm : most), kv_shared = kv + table <= most;
+#define SPA_REL_BWD(D, REL, REL_KV) bwd_launch<D, REL, REL_KV>(p, qkv, ao, lse, dao, seg, n_seg, dqkv, delta, rel, one_pass, d_status, st)
+#define SPA_REL_BWD_TABLES(D)                                                                               \
+  return dq_shared ? (kv_shared ? SPA_REL_BWD(D, kRelShared, kRelShared) : SPA_REL_BWD(D, kRelShared, kRelGlobal)) \
+                   : (kv_shared ? SPA_REL_BWD(D, kRelGlobal, kRelShared) : SPA_REL_BWD(D, kRelGlobal, kRelGlobal))
+  if (d64) SPA_REL_BWD_TABLES(64);
+  SPA_REL_BWD_TABLES(32);
+#undef SPA_REL_BWD_TABLES
 #undef SPA_REL_BWD
 }
 
