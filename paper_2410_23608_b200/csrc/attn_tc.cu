@@ -21,6 +21,7 @@
 
 #include "attn_rel.cuh"
 #include "attn_tc.cuh"
+#include "simt_stage.cuh"
 
 namespace spa {
 namespace {
@@ -739,7 +740,78 @@ template <int D, bool kDQ, int kRel = kNoRel> __host__ __device__ constexpr int 
          (kRel != kNoRel ? kBwdPosBytes : 0);
 }
 
-template <int D, bool kDQ, bool kLoop, int kRel>
+__device__ __forceinline__ int cluster_rank() {
+  int r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ int cluster_ctas() {
+  int n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+
+// Few items with many keys (or queries) each: the CTAs of a cluster take the streamed tiles of an item in parts of the same length, and
+// add up their accumulators over distributed shared memory, each an equal share of the item's rows, in the order of the parts: no
+// scratch, no second kernel, the same bits every time.  Accumulator a of this thread's row (columns acc_col[a] from tmem_at on) goes to the
+// tiles' memory as fp32, 16-byte chunks XORed by the row; what is not there (no tile for this part) counts as zeros.
+template <int D, int kAcc>
+__device__ void split_join(uint8_t* smem_al, uint32_t tmem_at, const uint32_t (&acc_col)[kAcc], bool is_math, bool there, int rl, int half,
+                           const volatile uint8_t* row_ok, __nv_bfloat16* dqkv, const int (&col)[kAcc], const float (&mul)[kAcc], int C, int r0, int h,
+                           const RelGrad& grad, bool keys) {
+  constexpr int kDh = D / 2, kRow = D * 4, kSize = 128 * kRow;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (is_math) {
+#pragma unroll
+    for (int a = 0; a < kAcc; ++a) {
+      uint32_t r[kDh];
+#pragma unroll
+      for (int e = 0; e < kDh; ++e) r[e] = 0u;
+      if (there) {
+        if (kDh == 32) ptx::tmem_ld_32x32(tmem_at + acc_col[a], r);
+        else ptx::tmem_ld_32x16(tmem_at + acc_col[a], r);
+        ptx::tmem_ld_wait();
+      }
+#pragma unroll
+      for (int g = 0; g < kDh / 4; ++g)
+        *reinterpret_cast<uint4*>(smem_al + a * kSize + rl * kRow + (((half * (kDh / 4) + g) ^ (rl & 7)) << 4)) =
+            make_uint4(r[4 * g], r[4 * g + 1], r[4 * g + 2], r[4 * g + 3]);
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();
+  const int parts = cluster_ctas(), share = 128 / parts, first = cluster_rank() * share;
+  for (int e = tid; e < share * (D / 8); e += kBwdThreads) {  // whole warps
+    const int r = first + e / (D / 8), c = e % (D / 8);
+    uint4 out[kAcc];
+    float sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < kAcc; ++a) {
+      float v[8];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float4 f = sum_dsmem4(reinterpret_cast<const float*>(smem_al + a * kSize + r * kRow + (((2 * c + g) ^ (r & 7)) << 4)), parts);
+        v[4 * g] = f.x * mul[a];
+        v[4 * g + 1] = f.y * mul[a];
+        v[4 * g + 2] = f.z * mul[a];
+        v[4 * g + 3] = f.w * mul[a];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += fabsf(v[i]);
+      out[a] = Vec16<__nv_bfloat16>::from_float(v);
+    }
+    // a half of a row that is not finite: see rel_redo
+    constexpr int kLanes = D / 16;
+    const unsigned bad = __ballot_sync(0xffffffffu, !(sum < CUDART_INF_F));
+    if (row_ok[r]) {
+#pragma unroll
+      for (int a = 0; a < kAcc; ++a) *reinterpret_cast<uint4*>(dqkv + (long long)(r0 + r) * 3 * C + col[a] + c * 8) = out[a];
+      if (c % kLanes == 0 && ((bad >> lane) & ((1u << kLanes) - 1u)) != 0u) rel_redo(grad, keys, c / kLanes, h, r0 + r);
+    }
+  }
+}
+
+template <int D, bool kDQ, bool kLoop, int kRel, bool kSplit = false>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
@@ -830,10 +902,10 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     for (int i = tid; i <= n_seg; i += kBwdThreads) seg_s[i] = ld_dep(seg + i);
   const int Np = packed_rows(seg, n_seg, capacity);
   const int n_items = ((Np + 127) / 128) * H;
-  if ((int)blockIdx.x >= n_items) return;
+  int item = kSplit ? (int)blockIdx.x / cluster_ctas() : (int)blockIdx.x;  // kSplit: one for all CTAs of a cluster
+  if (item >= n_items) return;
   if (skip_short) __syncthreads();  // the staged offsets are visible to the tile test
   bool cta_failed = false, first_item = true;
-  int item = blockIdx.x;
   do {  // kLoop: this CTA strides over the items; otherwise the grid holds one CTA per item and this is no loop
   const int h = item % H, r0 = (item / H) * 128;
   // tiles whose rows all belong to the one-pass kernel are passed over before anything is fetched
@@ -895,7 +967,13 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
   }
   __syncthreads();
   const bool any_row = range[1] > range[0];  // false: every row of the tile belongs to the one-pass kernel
-  const int o_lo = any_row ? range[0] : 0, o_hi = any_row ? range[1] : 0;
+  int o_lo = any_row ? range[0] : 0, o_hi = any_row ? range[1] : 0;
+  if (kSplit) {  // this CTA's part of them, in whole tiles
+    const int tiles = (o_hi - o_lo + kBwdY - 1) / kBwdY, first = tiles * cluster_rank() / cluster_ctas();
+    const int end = o_lo + tiles * (cluster_rank() + 1) / cluster_ctas() * kBwdY;
+    o_hi = end < o_hi ? end : o_hi;
+    o_lo += first * kBwdY;
+  }
   const int n_tiles = (o_hi - o_lo + kBwdY - 1) / kBwdY;
 
   const int y1_col = (kDQ ? C : 0) + h * D;           // streamed operand inside qkv: K | Q
@@ -1285,7 +1363,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
   ptx::tc_fence_after_sync();
   const bool failed = *abort_any != 0;
 
-  if (!failed && n_tiles > 0) {
+  if (!kSplit && !failed && n_tiles > 0) {
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
@@ -1325,18 +1403,25 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
       copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
       copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
     }
-    if constexpr (kRel != kNoRel) {
-      if (kDQ && rel.shared_bins) {  // the item's bins to the head's sums
-        const int shift = range[0];
-        rel_flush<kBwdThreads>(rel, reinterpret_cast<const int*>(bins), h, shift, tid);
-      }
-      if (again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
-    }
+    if (kRel != kNoRel && again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
   }
+  if (kRel != kNoRel && kDQ && !failed && n_tiles > 0 && rel.shared_bins)  // the item's bins to the head's sums
+    rel_flush<kBwdThreads>(rel, reinterpret_cast<const int*>(bins), h, range[0], tid);
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
     for (int t = issued > kStages ? issued - kStages : 0; t < issued; ++t) ptx::mbar_wait(bar_y(stage_of(t)), use_of(t));
     if (kDQ && issued < kStages) ptx::mbar_wait(bar_y(0), 0);  // the O tile, if no streamed tile followed it there
     ptx::mbar_wait(bar_x, 0);
+  }
+  if constexpr (kSplit) {
+    __syncthreads();  // the tiles' memory is free
+    const uint32_t at = tmem + lane_base + half * (D / 2);
+    if constexpr (kDQ)
+      split_join<D, 1>(smem_al, at, {kColAcc1}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv, {h * D}, {scale}, C, r0, h, rel.grad, false);
+    else
+      split_join<D, 2>(smem_al, at, {kColAcc1, kColAcc2}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv, {2 * C + h * D, C + h * D},
+                       {1.f, scale}, C, r0, h, rel.grad, true);
+    __syncwarp();
+    cluster_sync_all();  // nobody leaves while its accumulators are still being read
   }
   cta_failed = failed;
   ptx::tc_fence_before_sync();
@@ -1362,7 +1447,7 @@ template <int D, int kRel = kNoRel> __host__ __device__ constexpr int split_smem
          (kRel != kNoRel ? kBwdPosBytes : 0);
 }
 
-template <int D, bool kLoop, int kRel>
+template <int D, bool kLoop, int kRel, bool kSplit = false>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
@@ -1446,10 +1531,10 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     for (int i = tid; i <= n_seg; i += kBwdThreads) seg_s[i] = ld_dep(seg + i);
   const int Np = packed_rows(seg, n_seg, capacity);
   const int n_items = ((Np + 127) / 128) * H;
-  if ((int)blockIdx.x >= n_items) return;
+  int item = kSplit ? (int)blockIdx.x / cluster_ctas() : (int)blockIdx.x;  // kSplit: one for all CTAs of a cluster
+  if (item >= n_items) return;
   if (skip_short) __syncthreads();  // the staged offsets are visible to the tile test
   bool cta_failed = false, first_item = true;
-  int item = blockIdx.x;
   do {  // kLoop: this CTA strides over the items; otherwise the grid holds one CTA per item and this is no loop
   const int h = item % H, r0 = (item / H) * 128;
   // tiles whose rows all belong to the one-pass kernel are passed over before anything is fetched
@@ -1500,7 +1585,13 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
   }
   __syncthreads();
   const bool any_row = range[1] > range[0];  // false: every row of the tile belongs to the one-pass kernel
-  const int o_lo = any_row ? range[0] : 0, o_hi = any_row ? range[1] : 0;
+  int o_lo = any_row ? range[0] : 0, o_hi = any_row ? range[1] : 0;
+  if (kSplit) {  // this CTA's part of them, in whole tiles
+    const int tiles = (o_hi - o_lo + kBwdY - 1) / kBwdY, first = tiles * cluster_rank() / cluster_ctas();
+    const int end = o_lo + tiles * (cluster_rank() + 1) / cluster_ctas() * kBwdY;
+    o_hi = end < o_hi ? end : o_hi;
+    o_lo += first * kBwdY;
+  }
   const int n_tiles = (o_hi - o_lo + kBwdY - 1) / kBwdY;
 
   const int y1_col = h * D;                           // streamed operand inside qkv: Q
@@ -1796,7 +1887,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
   ptx::tc_fence_after_sync();
   const bool failed = *abort_any != 0;
 
-  if (!failed && n_tiles > 0) {
+  if (!kSplit && !failed && n_tiles > 0) {
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
@@ -1835,6 +1926,13 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
     for (int t = issued > kStages ? issued - kStages : 0; t < issued; ++t) ptx::mbar_wait(bar_y(stage_of(t)), use_of(t));
     ptx::mbar_wait(bar_x, 0);
+  }
+  if constexpr (kSplit) {
+    __syncthreads();  // the tiles' memory is free
+    split_join<D, 2>(smem_al, tmem + lane_base + half * (D / 2), {kColAcc1, kColAcc2}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv,
+                     {2 * C + h * D, C + h * D}, {1.f, scale}, C, r0, h, rel.grad, true);
+    __syncwarp();
+    cluster_sync_all();  // nobody leaves while its accumulators are still being read
   }
   cta_failed = failed;
   ptx::tc_fence_before_sync();
@@ -2082,13 +2180,44 @@ attn_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_c
 template <int D, int kRel> struct kv_pass {
   static constexpr int kThreads = kBwdThreads;
   static constexpr int kSmem = bwd_smem_bytes<D, false, kRel>();
-  template <bool kLoop> static auto kernel() { return attn_bwd_tc_kernel<D, false, kLoop, kRel>; }
+  template <bool kLoop, bool kSplit = false> static auto kernel() { return attn_bwd_tc_kernel<D, false, kLoop, kRel, kSplit>; }
 };
 template <int kRel> struct kv_pass<64, kRel> {
   static constexpr int kThreads = kBwdThreads;
   static constexpr int kSmem = split_smem_bytes<64, kRel>();
-  template <bool kLoop> static auto kernel() { return attn_bwd_kv_split_kernel<64, kLoop, kRel>; }
+  template <bool kLoop, bool kSplit = false> static auto kernel() { return attn_bwd_kv_split_kernel<64, kLoop, kRel, kSplit>; }
 };
+
+// CTAs to an item of the backward with a bias: as many as all run at once, while each has two streamed tiles or more of a segment, which
+// is of one image.  Backward, us, one CTA -> these: one image of 47 x 83, one head of 64, 250 -> 94, of 40 x 60, two of 32, 143 -> 83, two of
+// 24 x 24, 12 of 64, 83 -> 65.  A quarter more CTAs than run at once: 83 -> 97 for the second; one streamed tile each: one image of 24 x 24 with half
+// of it selected, 12 heads of 64, 43 -> 65.
+int rel_parts(const spa_params& p, int smem) {
+  const long long items = (long long)p.H * ((p.capacity + 127) / 128), slots = kNumSMs * (smem <= kTwoPerSm ? 2 : 1);
+  const int rows = p.N < p.capacity ? p.N : p.capacity;
+  int parts = 1;
+  while (parts < 8 && 2 * parts * items <= slots && 2 * kBwdY * 2 * parts <= rows) parts *= 2;
+  return parts;
+}
+
+// launch_pdl with `cluster` CTAs to a cluster
+template <typename... KArgs, typename... Args>
+cudaError_t launch_cluster(void (*kern)(KArgs...), int grid, int cluster, size_t smem, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kBwdThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
 
 // kRel, kRelKV: rel is used by the dQ and by the dK / dV pass, and the memory that the tables need is added to the kernels' own.  The
 // bins of the dQ pass come first (kRelGlobal: they may take a whole SM's memory), then the table.
@@ -2139,6 +2268,27 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
   auto kq = loop ? attn_bwd_tc_kernel<D, true, true, kRel> : attn_bwd_tc_kernel<D, true, false, kRel>;
   auto kkv = loop ? KV::template kernel<true>() : KV::template kernel<false>();
   const float scale = softmax_scale_of(p);
+  if constexpr (kRel != kNoRel) {
+    const int dq_parts = rel_parts(p, dq_smem), kv_parts = rel_parts(p, kv_smem);
+    if (dq_parts * kv_parts > 1 && !loop) {
+      auto sq = attn_bwd_tc_kernel<D, true, false, kRel, true>;
+      auto skv = KV::template kernel<false, true>();
+      static DeviceOnce split_attr;
+      cudaError_t es = split_attr.run([&] {
+        const cudaError_t e = cudaFuncSetAttribute(sq, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSm);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(skv, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSm);
+      });
+      if (es == cudaSuccess)
+        es = launch_cluster(sq, grid * dq_parts, dq_parts, dq_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg, n_seg, p.capacity, p.C,
+                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, d_status);
+      if (es == cudaSuccess)
+        es = launch_cluster(skv, grid * kv_parts, kv_parts, kv_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg, n_seg, p.capacity, p.C,
+                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, d_status);
+      if (es != cudaSuccess) { set_cuda_error(es, "attn_bwd_tc_kernel"); return SPA_ERR_CUDA; }
+      SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dKV)");
+      return SPA_OK;
+    }
+  }
   // Under SPA_FLAG_ONE_PASS_BWD segments of at most 128 rows go to the one-pass kernel (one CTA per segment and
   // head) and the two passes take the longer ones; otherwise, or with more segments than a grid dimension holds, the
   // two passes take everything.

@@ -89,6 +89,33 @@ def test_values_that_are_not_finite_stay_in_their_segment(dtype, d, flags, grid,
     assert torch.isfinite(run.dtable[:, 1]).all()
 
 
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("grid,counts", [((17, 16), (272,)), ((17, 16), (1, 200)), ((24, 25), (600, 3)), ((24, 25), (64, 65, 300)), ((33, 40), (1320,)),
+                                         ((33, 40), (129, 1000)), ((33, 40), (0, 30, 0, 700))])
+@pytest.mark.parametrize("H", [1, 3])
+def test_few_long_segments(dtype, d, flags, grid, counts, H):
+    """Few row tiles with many keys each: the keys of a tile are dealt to several CTAs, of which some may get none."""
+    check(Run(problem(dtype, d, H, *grid, counts, seed=sum(counts) + H), flags), flags)
+
+
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("what", ["q", "k", "v", "d_out"])
+def test_infinities_in_one_of_few_long_segments(dtype, d, flags, what):
+    pr = problem(dtype, d, 1, 33, 40, (700, 300), seed=5)
+    clean, run = Run(pr, flags), Run(pr, flags)
+    if what == "d_out":
+        run.d_out[720, 1] = float("inf")
+    else:
+        run.qkv[720, {"q": 0, "k": 1, "v": 2}[what] * pr["C"] + 1] = float("inf")
+    for r in (clean, run):
+        r.fwd(); r.bwd()
+    torch.cuda.synchronize()
+    for k in ("out", "dqkv"):
+        a, b = host(getattr(run, k))[:700], host(getattr(clean, k))[:700]
+        tol = (4 * W if dtype == "bf16" else 64 * U) * np.abs(b).max()
+        assert np.isfinite(a).all() and np.abs(a - b).max() <= tol, (k, np.abs(a - b).max() / tol)
+
+
 def test_rows_beyond_four_gigabytes():
     """2^20 packed rows of 2 304 bf16 values: places past 2^31 elements and 2^32 bytes, in segments of 64."""
     from paper_2410_23608_b200 import binding as L
