@@ -23,10 +23,10 @@ struct Prep {
   const int32_t *bucket, *idx, *seg;
   const void *qkv, *dao;  // backward only
   float* bias;
-  int32_t *pos, *owner, *bad;
+  int32_t *pos, *owner, *bad, *place;
   uint32_t* redo;
   unsigned* counters;
-  unsigned long long* acc;
+  unsigned long long *acc, *acc_off;
   float* bound;
   int n_seg, capacity, B, N, rows, cols, n_buckets, entries, pitch, C, H;
   float mul;
@@ -76,6 +76,11 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   }
   if constexpr (kBwd) {
     for (int i = tid; i < a.n_buckets * a.H; i += all) a.acc[i] = 0ull;
+    if (a.acc_off != nullptr)
+      for (int i = tid; i < a.pitch * a.H; i += all) {
+        a.acc_off[i] = 0ull;
+        if (i < a.pitch) a.place[i] = i;
+      }
     for (int i = tid; i < a.H; i += all) a.bad[i] = 0;
     __syncthreads();
     // A thread has one chunk of a row, the same one of every row it looks at, and neighbouring lanes the other chunks of its head:
@@ -173,10 +178,32 @@ __device__ void redo_row(const Redo& r, const int32_t* seg, int n_seg, int capac
   }
 }
 
+// Sums by offset to the buckets' (see rel_few_buckets).  Neighbouring offsets are mostly of one bucket: a warp adds such up first.
+__global__ void __launch_bounds__(256) rel_fold_kernel(const unsigned long long* off, unsigned long long* acc, const int32_t* bucket, int entries,
+                                                       int pitch, int n_buckets, int H) {
+  pdl_entry();
+  const int lane = threadIdx.x & 31, all = gridDim.x * 256;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i - lane < pitch * H; i += all) {  // whole warps
+    const int h = i / pitch, at = i % pitch;
+    const bool in = i < pitch * H && at < entries;
+    const int b = in ? bucket[at] : -1, key = in && (unsigned)b < (unsigned)n_buckets ? h * n_buckets + b : -1;
+    unsigned long long v = key >= 0 ? off[i] : 0ull;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {  // the first lane of 2 o takes what the first of their second half has
+      const unsigned long long w = __shfl_xor_sync(0xffffffffu, v, o);
+      if (__shfl_xor_sync(0xffffffffu, key, o) == key) {
+        if ((lane & (2 * o - 1)) == 0) v += w;
+        else if ((lane & (2 * o - 1)) == o) v = 0ull;
+      }
+    }
+    if (v != 0ull) atomicAdd(acc + key, v);
+  }
+}
+
 // dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.  kRedo: behind
 // the tensor-core kernels, the rows that they noted down.
 template <bool kRedo>
-__global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const Redo r, const int32_t* seg, int n_seg, int capacity,
+__global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const unsigned long long* acc, int n_buckets, const Redo r, const int32_t* seg, int n_seg, int capacity,
                                                          const int32_t* idx, const int32_t* owner, int tokens,
                                                          float* __restrict__ dtable, int32_t* d_status) {
   pdl_entry();
@@ -189,9 +216,9 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
   }
   __syncthreads();
   const int tid = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
-  for (int i = tid; i < g.n_buckets * g.H; i += all) {
+  for (int i = tid; i < n_buckets * g.H; i += all) {
     const int h = i % g.H;
-    dtable[i] = (float)((double)(long long)g.acc[(long long)h * g.n_buckets + i / g.H] * (double)unit[h]);
+    dtable[i] = (float)((double)(long long)acc[(long long)h * n_buckets + i / g.H] * (double)unit[h]);
   }
   const int Np = packed_rows(seg, n_seg, capacity);
   for (int i = tid; i < Np; i += all) {
@@ -207,8 +234,9 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Layout {
-  size_t pos, bias, acc, bound, bad, owner, delta, redo, end;
+  size_t pos, bias, acc, acc_off, place, bound, bad, owner, delta, redo, end;
   int entries, pitch, center;
+  bool few;
 };
 Layout layout(const spa_params& p, const spa_rel_bias& r) {
   Layout l;
@@ -221,6 +249,9 @@ Layout layout(const spa_params& p, const spa_rel_bias& r) {
   l.pos = take(((size_t)p.capacity + 128) * 4);
   l.bias = take((size_t)p.H * l.pitch * 4);
   l.acc = take((size_t)r.n_buckets * p.H * 8);
+  l.few = rel_few_buckets(l.entries, r.n_buckets);
+  l.acc_off = take(l.few ? (size_t)l.pitch * p.H * 8 : 0);
+  l.place = take(l.few ? (size_t)l.pitch * 4 : 0);
   l.bound = take((size_t)kRelBlocks * p.H * 8);
   l.bad = take((size_t)p.H * 4);
   l.owner = take((size_t)p.B * p.N * 4);
@@ -250,6 +281,8 @@ int launch_prep(const spa_params& p, const spa_rel_bias& r, const Layout& l, cha
   a.redo = (uint32_t*)(ws + l.redo);
   a.counters = (unsigned*)(ws + l.bad);  // forward and backward use one or the other
   a.acc = (unsigned long long*)(ws + l.acc);
+  a.acc_off = l.few ? (unsigned long long*)(ws + l.acc_off) : nullptr;
+  a.place = (int32_t*)(ws + l.place);
   a.bound = (float*)(ws + l.bound);
   a.n_seg = n_seg;
   a.capacity = p.capacity;
@@ -307,24 +340,30 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, qkv, dao, tc ? kLog2e : 1.f, d_status, st);
   if (rc != SPA_OK) return rc;
   RelGrad g = {};
-  g.acc = (unsigned long long*)(ws + l.acc);
-  g.bucket = r.bucket;
+  unsigned long long* acc = (unsigned long long*)(ws + l.acc);
+  g.acc = l.few ? (unsigned long long*)(ws + l.acc_off) : acc;
+  g.place = l.few ? (const int32_t*)(ws + l.place) : r.bucket;
+  g.places = l.few ? l.pitch : r.n_buckets;
   g.bound = (const float*)(ws + l.bound);
   g.peak = peak;
   g.bad = (int32_t*)(ws + l.bad);
   g.redo = (uint32_t*)(ws + l.redo);
-  g.n_buckets = r.n_buckets;
   g.H = p.H;
   g.most_redo = 4u * p.H * p.capacity;
   rc = tc ? launch_attention_rel_bwd_tc(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, (float*)(ws + l.delta), d_status, st)
           : launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);
   if (rc != SPA_OK) return rc;
+  if (l.few) {
+    const int ctas = (l.pitch * p.H + 255) / 256;
+    launch_pdl(rel_fold_kernel, ctas < 4 * kNumSMs ? ctas : 4 * kNumSMs, 256, 0, st, g.acc, acc, r.bucket, l.entries, l.pitch, r.n_buckets, p.H);
+    SPA_CUDA_CHECK_LAUNCH("rel_fold_kernel");
+  }
   const long long work = (long long)r.n_buckets * p.H > p.capacity ? (long long)r.n_buckets * p.H : p.capacity;
   // behind the tensor-core kernels a CTA per SM, should there be rows to form again
   const int grid = (int)(!tc && (work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
   const Redo redo{view(l, ws), (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, lse, (const float*)(ws + l.delta), (__nv_bfloat16*)dqkv,
                p.C, p.C / p.H, softmax_scale_of(p)};
-  launch_pdl(tc ? rel_finish_kernel<true> : rel_finish_kernel<false>, grid, 256, (size_t)p.H * sizeof(float), st, g, redo, seg, n_seg, p.capacity,
+  launch_pdl(tc ? rel_finish_kernel<true> : rel_finish_kernel<false>, grid, 256, (size_t)p.H * sizeof(float), st, g, acc, r.n_buckets, redo, seg, n_seg, p.capacity,
              idx, (const int32_t*)(ws + l.owner), p.B * p.N, dtable, d_status);
   SPA_CUDA_CHECK_LAUNCH("rel_finish_kernel");
   return SPA_OK;

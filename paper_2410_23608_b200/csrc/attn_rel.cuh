@@ -33,13 +33,15 @@ __device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int
 
 constexpr int kRelBlocks = kNumSMs;  // CTAs of the kernel that prepares a call, each with its own maxima
 struct RelGrad {
-  unsigned long long* acc;  // [H][n_buckets] sums of dS times 2^(kRelBits - exponent of the head's bound)
-  const int32_t* bucket;    // [entries]
+  // [H][places] sums of dS times 2^(kRelBits - exponent of the head's bound): a place for each bucket, or, where they are few
+  // (rel_few_buckets), one for each offset, and rel_fold_kernel behind the attention
+  unsigned long long* acc;
+  const int32_t* place;  // [entries]: the buckets, or the offsets themselves (a NULL for these, and a branch, made the dQ pass 3 % slower)
   const float* bound;       // [kRelBlocks][H][2] largest |v_j|^2 and |dO_i|^2
   const float* peak;        // [H][capacity] log of the row's largest probability, optional
   int32_t* bad;             // [H] a row's statistics are not finite
   uint32_t* redo;           // [1 + 4 H capacity] how many, and which parts of rows are to be formed again
-  int n_buckets, H;
+  int places, H;
   uint32_t most_redo;       // 4 H capacity
 };
 
@@ -94,11 +96,15 @@ __device__ __forceinline__ void rel_check_row(const RelGrad& g, int h, float lse
   if (!(lse < __uint_as_float(0x7f800000u)) || !(fabsf(D) < __uint_as_float(0x7f800000u))) g.bad[h] = 1;
 }
 
-// v to the bin of the bucket of table entry `at`
+// v to the place of table entry `at`
 __device__ __forceinline__ void rel_add(const RelGrad& g, int h, int at, long long v) {
-  const int b = g.bucket[at];
-  if ((unsigned)b < (unsigned)g.n_buckets && v != 0) atomicAdd(g.acc + (long long)h * g.n_buckets + b, (unsigned long long)v);
+  const int b = g.place[at];
+  if ((unsigned)b < (unsigned)g.places && v != 0) atomicAdd(g.acc + (long long)h * g.places + b, (unsigned long long)v);
 }
+// Few buckets for many offsets: atomics of all CTAs would queue for the few sums.  us, places by bucket -> by offset, with 25 buckets: 128
+// images of 14 x 14 with 30 to 60 % selected, 12 heads of 64, 146 -> 114, 512 windows of 7 x 7 (6.8 offsets to a bucket), 12 heads of 32, 102 -> 94, fp32 64
+// images of 14 x 14, 6 heads of 64, 1178 -> 313.  Folding costs 1 to 2 us: with 225 buckets the first takes 111 either way.
+inline bool rel_few_buckets(int entries, int n_buckets) { return entries >= 4 * (long long)n_buckets; }
 
 // What the kernels with a bias by relative position are given beside the others' arguments.  shared_bins: the table's gradient is
 // summed in shared memory, item by item; else pair by pair in global memory.
@@ -152,12 +158,12 @@ __device__ __forceinline__ void rel_flush(const RelBwd& rel, const int* bins, in
     for (int u = 0; u < 4; ++u) {
       const int at = i + u * kThreads;
       v[u] = at < rel.view.entries ? ((long long)bins[rel.view.pitch + at] << kRelLow) + bins[at] : 0;
-      b[u] = v[u] != 0 ? rel.grad.bucket[at] : -1;
+      b[u] = v[u] != 0 ? rel.grad.place[at] : -1;
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if ((unsigned)b[u] < (unsigned)rel.grad.n_buckets)
-        atomicAdd(rel.grad.acc + (long long)h * rel.grad.n_buckets + b[u], (unsigned long long)rel_shifted(v[u], shift));
+      if ((unsigned)b[u] < (unsigned)rel.grad.places)
+        atomicAdd(rel.grad.acc + (long long)h * rel.grad.places + b[u], (unsigned long long)rel_shifted(v[u], shift));
   }
 }
 
