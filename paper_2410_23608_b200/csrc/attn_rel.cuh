@@ -123,6 +123,17 @@ __device__ __forceinline__ void rel_bin(uint32_t at, uint32_t pitch_bytes, float
   ptx::red_add_s32(at, v & ((1 << kRelLow) - 1));
   ptx::red_add_s32(at + pitch_bytes, v >> kRelLow);
 }
+// The fp32-FMA kernels: 42 bits of a pair in three words, 14 bits to each of the lower two; 32 query rows
+constexpr int kRelThird = 14;
+__device__ __forceinline__ void rel_bin3(int* bin, int pitch, long long v) {
+  atomicAdd(bin, (int)v & ((1 << kRelThird) - 1));
+  atomicAdd(bin + pitch, (int)(v >> kRelThird) & ((1 << kRelThird) - 1));
+  atomicAdd(bin + 2 * pitch, (int)(v >> 2 * kRelThird));
+}
+template <int kThreads> __device__ __forceinline__ void rel_flush3(const RelGrad& g, const int* bins, int entries, int pitch, int h, int tid) {
+  for (int i = tid; i < entries; i += kThreads)
+    rel_add(g, h, i, ((long long)bins[2 * pitch + i] << 2 * kRelThird) + ((long long)bins[pitch + i] << kRelThird) + bins[i]);
+}
 // A sum in units of an item's scale as one in units of the head's
 __device__ __forceinline__ long long rel_shifted(long long v, int shift) {
   return shift >= 0 ? v << shift : v >> (shift > -63 ? -shift : 63);

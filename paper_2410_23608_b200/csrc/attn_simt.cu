@@ -323,7 +323,7 @@ attn_fwd_simt_kernel(const T* qkv, const int32_t* seg, int n_seg, int capacity, 
 // blockIdx.z = 1: own rows are keys, streamed rows queries, everything transposed: dV += P^T dO, dK += dS^T Q.
 template <int D, int kGroups> constexpr int kBwdFloats = (2 * kR + kGroups * 2 * kT) * kLd<D> + kGroups * (kR * kLdP + 2 * kT);
 
-template <typename T, int D, int kGroups, bool kRel>
+template <typename T, int D, int kGroups, bool kRel, bool kBins>
 __global__ void __launch_bounds__(kGroups * kGroup, 4 / kGroups)
 attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
                      const T* dao, const int32_t* seg, int n_seg, int capacity, int C,
@@ -408,6 +408,9 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
       if (r < Np) rel_check_row(grad, h, lv, dv);
     }
   }
+  int* bins = reinterpret_cast<int*>(sm + kBwdFloats<D, kGroups>);
+  if (kBins && dq)
+    for (int i = threadIdx.x; i < 3 * rel.pitch; i += kThreads) bins[i] = 0;
   float acc1[4][W] = {}, acc2[4][W] = {};  // dQ | dK and dV
   own_rows_landed<1>(grp < n_tiles);
   for (int t = grp; t < n_tiles; t += kGroups) {
@@ -436,7 +439,11 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
           p = in && l != -CUDART_INF_F ? expf(fmaf(s[i][j], scale, bias[off]) - l) : 0.f;  // no key: no weight
           if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
           dp[i][j] = in ? p * (dp[i][j] - Dv) : 0.f;
-          if (dq && in) rel_add(grad, h, off + rel.center, __float2ll_rn(dp[i][j] * table_scale));
+          if (dq && in) {
+            const long long v = __float2ll_rn(dp[i][j] * table_scale);
+            if (kBins) rel_bin3(bins + off + rel.center, rel.pitch, v);
+            else rel_add(grad, h, off + rel.center, v);
+          }
         } else {
           p = in ? expf(s[i][j] * scale - l) : 0.f;
           if (!dq) Ps[(ty + kTY * i) * kLdP + c] = p;
@@ -484,6 +491,8 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
         acc2[i][d] += part[((4 + i) * W + d) * kGroup];
       }
   }
+  // behind a barrier of all threads that have added to the bins
+  if (kBins && dq) rel_flush3<kGroup>(grad, bins, rel.entries, rel.pitch, h, tid);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = i0 + ty + kTY * i;
@@ -514,6 +523,11 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
   }
 }
 
+// Offsets up to which a CTA sums the table's gradient in shared memory and adds it to the head's behind its tiles: with few, the atomics of
+// all CTAs meet on the same lines (256 windows of 7 x 7, 169 offsets, 6 heads of 32, 311 -> 196 us); with many, a CTA's 32 rows add to them about as
+// often as they are many (64 images of 14 x 14, 729 offsets, 6 heads of 64, 311 -> 319; 30 of 10 x 12, 437, 44 either way).
+constexpr int kMostBins = 256;
+
 template <typename T, int D, int kGroups, bool kRel>
 int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
                float* peak, cudaStream_t st) {
@@ -531,12 +545,17 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
 template <typename T, int D, int kGroups, bool kRel>
 int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                const int32_t* seg, int n_seg, const RelView& rel, const RelGrad& grad, void* dqkv, cudaStream_t st) {
-  auto kern = attn_bwd_simt_kernel<T, D, kGroups, kRel>;
-  constexpr int kSmem = kBwdFloats<D, kGroups> * (int)sizeof(float);
+  constexpr int kSmem = kBwdFloats<D, kGroups> * (int)sizeof(float), kBins = 12 * kMostBins;
+  auto with_bins = attn_bwd_simt_kernel<T, D, kGroups, kRel, kRel>, without = attn_bwd_simt_kernel<T, D, kGroups, kRel, false>;
+  const bool bins = kRel && rel.pitch <= kMostBins;
+  auto kern = bins ? with_bins : without;
   static DeviceOnce attr;
-  cudaError_t e = attr.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+  cudaError_t e = attr.run([&] {
+    const cudaError_t first = cudaFuncSetAttribute(without, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    return !kRel || first != cudaSuccess ? first : cudaFuncSetAttribute(with_bins, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem + kBins);
+  });
   if (e != cudaSuccess) { set_cuda_error(e, "attn_bwd_simt_kernel"); return SPA_ERR_CUDA; }
-  launch_pdl(kern, dim3((p.capacity + kR - 1) / kR, p.H, 2), kGroups * kGroup, kSmem, st, (const T*)qkv, (const T*)ao, lse,
+  launch_pdl(kern, dim3((p.capacity + kR - 1) / kR, p.H, 2), kGroups * kGroup, kSmem + (bins ? kBins : 0), st, (const T*)qkv, (const T*)ao, lse,
              (const T*)dao, seg, n_seg, p.capacity, p.C, softmax_scale_of(p), rel, grad, (T*)dqkv);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_simt_kernel");
   return SPA_OK;
