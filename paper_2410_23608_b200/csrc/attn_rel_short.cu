@@ -9,7 +9,8 @@
 // and dS to the bins of the table's gradient, as in the dQ pass.  Two threads share a row, 64 columns each in groups of 32, and a warp
 // passes over the groups that none of its rows has columns in.  A tile's steps follow one another and two CTAs share an SM, so
 // that one computes while the other waits.  A CTA takes a few segments of one head at a time and tiles them itself.
-// 512 windows of 7 x 7, 12 heads of 32, two passes -> one: see launch_attention_rel_bwd_short.
+// What bounds it is the chain of a tile's steps: 512 windows of 7 x 7, 12 heads of 32, 91 us against 24 for their bytes, issue slots half
+// full, the memory a fifth.
 #include <math_constants.h>
 
 #include "attn_rel.cuh"
@@ -804,6 +805,10 @@ int launch(const spa_params& p, const void* qkv, const void* ao, const float* ls
 
 }  // namespace
 
+// Backward, us, two passes -> one pass (and the two for longer segments): 512 windows of 7 x 7, 12 heads of 32, 228 -> 124, of two to a tile
+// 91; of 64, 288 -> 163 -> 155; 128 images of 10 x 10, 12 heads of 64, 173 -> 92; of 14 x 14 with 5 to 60 % selected 105 -> 96.  The line counts rows of
+// the capacity, since the host does not know the segments: where they are longer than 128 after all, images of 14 x 14 with 60 to 100 %
+// selected, 280 -> 315, all 370 -> 382.
 bool attention_rel_bwd_short_applies(const spa_params& p, int n_seg, const RelView& view) {
   const int base = p.C / p.H == 64 ? Smem<64>::kBytes : Smem<32>::kBytes;
   return n_seg >= 1 && (long long)p.capacity <= 256ll * n_seg && base + 3 * view.pitch * 4 <= kTwoPerSm;
@@ -812,7 +817,9 @@ bool attention_rel_bwd_short_applies(const spa_params& p, int n_seg, const RelVi
 int launch_attention_rel_bwd_short(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                                    const int32_t* seg, int n_seg, const RelBwd& rel, void* dqkv, float* delta, int32_t* d_status,
                                    cudaStream_t st) {
-  // two to a tile where most segments are of at most 64 rows and the tables fit; a segment is of one image, which may rule out longer ones
+  // Two to a tile where most segments are of at most 64 rows and the tables fit (124 -> 91 and 163 -> 155 above; one image per segment and
+  // 64 rows or less on average would take in selections of which half are longer: 128 images of 14 x 14 110 -> 155).  A segment is of one
+  // image, which may rule out longer ones.
   const bool d64 = p.C / p.H == 64;
   const bool pairs = (p.N <= kPairMax || (n_seg >= 2 * p.B && (long long)p.capacity <= (long long)kPairMax * n_seg)) &&
                      (d64 ? PairSmem<64>::kBytes <= PairSmem<64>::kMost - 3 * rel.view.pitch * 4

@@ -116,6 +116,25 @@ def test_infinities_in_one_of_few_long_segments(dtype, d, flags, what):
         assert np.isfinite(a).all() and np.abs(a - b).max() <= tol, (k, np.abs(a - b).max() / tol)
 
 
+@pytest.mark.parametrize("dtype,d,flags", KINDS)
+@pytest.mark.parametrize("grid,counts,nb", [((33, 40), (700, 300), None), ((33, 40), (1320,), 7), ((7, 7), (49, 49, 30, 49), 5), ((14, 14), [150] * 12, 9)])
+def test_reproducible_in_a_graph(dtype, d, flags, grid, counts, nb):
+    """Split items, and sums by offset that are folded into few buckets: the same bits with every replay, and those of the call alone."""
+    run = Run(problem(dtype, d, 2, *grid, counts, nb=nb, seed=3), flags)
+    run.fwd(); run.bwd()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (run.dqkv, run.dtable)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run.fwd(); run.bwd()
+    for _ in range(5):
+        run.ws.fill_(0x55)
+        run.dqkv.fill_(Run.GUARD); run.dtable.fill_(5.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(run.dqkv, want[0]) and torch.equal(run.dtable, want[1])
+
+
 def test_rows_beyond_four_gigabytes():
     """2^20 packed rows of 2 304 bf16 values: places past 2^31 elements and 2^32 bytes, in segments of 64."""
     from paper_2410_23608_b200 import binding as L

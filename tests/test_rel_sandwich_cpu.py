@@ -201,6 +201,12 @@ def test_python_side_refusals(lib):
         lib.rel_bias(3, 4, cpu, torch.zeros(4, 2))           # a bucket for every offset
     with pytest.raises(ValueError):
         lib.rel_bias(3, 5, cpu.long(), torch.zeros(4, 2))
+    with pytest.raises(ValueError):
+        lib.sandwich("layer", "score", gate=torch.zeros(4, dtype=torch.bfloat16))  # scores are fp32
+    with pytest.raises(ValueError):
+        lib.sandwich("layer", "score")
+    with pytest.raises(ValueError):
+        lib.sandwich("rms", "image", gate=torch.zeros(4, 8))  # a host tensor
 
 
 def test_struct_layouts(lib):
