@@ -11,9 +11,6 @@ namespace spa {
 namespace {
 
 constexpr int kPrepThreads = 512;
-// Entries below this mask: beside any other they have no weight, and where a row has nothing else, its logarithm of the sum would have no bits
-// left for S (a type's lowest value times log2 e is not even finite).  Such rows are rows without a key.
-constexpr float kMasked = -1e6f;
 constexpr float kLog2e = 1.4426950408889634f;  // the tensor-core kernels take exponentials in base 2
 
 bool use_tc(const spa_params& p) { return !(p.flags & SPA_FLAG_SIMT_ONLY) && tc_attention_fwd_supported(p); }
@@ -44,33 +41,22 @@ __global__ void __launch_bounds__(kPrepThreads) rel_prep_kernel(const Prep a, in
   if (kBwd)
     for (int i = threadIdx.x; i < 2 * a.H; i += kPrepThreads) top[i] = 0u;
   const int Np = packed_rows(a.seg, a.n_seg, a.capacity);
-  if (tid == 0) *a.redo = 0u;
+  if (kBwd && tid == 0) *a.redo = 0u;
   if (!kBwd)
     for (int h = tid; h < a.H; h += all) a.counters[h] = 0u;
   for (int o = tid; o < a.pitch; o += all) {
     const int b = o < a.entries ? a.bucket[o] : 0;
     const bool ok = (unsigned)b < (unsigned)a.n_buckets;
     if (!ok) record_status(d_status, SPA_ERR_INVALID_ARG);
-    for (int h = 0; h < a.H; ++h) {
-      float v = ok ? to_f32<T>(table[(long long)b * a.H + h]) : 0.f;
-      if (v < kMasked) v = -CUDART_INF_F;
-      a.bias[(long long)h * a.pitch + o] = v * a.mul;
-    }
+    for (int h = 0; h < a.H; ++h)
+      a.bias[(long long)h * a.pitch + o] = rel_entry(ok ? to_f32<T>(table[(long long)b * a.H + h]) : 0.f, a.mul);
   }
   for (int i = tid; i < a.capacity + 128; i += all) {
     int p = 0;
     if (i < Np) {
-      const int t = ld_dep(a.idx + i);
-      if ((unsigned)t < (unsigned)(a.B * a.N)) {
-        const int n = t % a.N;
-        p = n / a.cols * (2 * a.cols - 1) + n % a.cols;
-        if (kBwd) a.owner[t] = i;
-        // a segment holds tokens of one image
-        const int before = i > 0 ? ld_dep(a.idx + i - 1) : t;
-        if (t / a.N != before / a.N && ld_dep(a.seg + find_segment(a.seg, a.n_seg, i)) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
-      } else {
-        record_status(d_status, SPA_ERR_INVALID_ARG);
-      }
+      const int t = ld_dep(a.idx + i), before = i > 0 ? ld_dep(a.idx + i - 1) : t;
+      p = rel_position(t, before, i, a.N, a.cols, a.B * a.N, [&] { return ld_dep(a.seg + find_segment(a.seg, a.n_seg, i)); }, d_status);
+      if (kBwd && (unsigned)t < (unsigned)(a.B * a.N)) a.owner[t] = i;
     }
     a.pos[i] = p;
   }
@@ -325,9 +311,13 @@ int launch_attention_rel_fwd(const spa_params& p, const spa_rel_bias& r, const v
   const Layout l = layout(p, r);
   char* ws = static_cast<char*>(workspace);
   const bool tc = use_tc(p);
+  if (tc && attention_rel_fwd_prepares(p, l.pitch)) {
+    const RelRaw raw{idx, r.bucket, r.table, r.cols, p.N, p.B * p.N, r.n_buckets};
+    return launch_attention_rel_fwd_tc(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, &raw, d_status, st);
+  }
   int rc = launch_prep(p, r, l, ws, seg, n_seg, idx, nullptr, nullptr, tc ? kLog2e : 1.f, d_status, st);
   if (rc != SPA_OK) return rc;
-  if (tc) return launch_attention_rel_fwd_tc(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, d_status, st);
+  if (tc) return launch_attention_rel_fwd_tc(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, nullptr, d_status, st);
   return launch_attention_rel_fwd_simt(p, qkv, seg, n_seg, view(l, ws), ao, lse, peak, st);
 }
 

@@ -23,10 +23,33 @@ struct RelView {          // what the forward and backward kernels read
   int pitch, entries, center;
 };
 
+// What the preparation works from, for a forward kernel that does it itself
+struct RelRaw {
+  const int32_t *idx, *bucket;
+  const void* table;
+  int cols, N, tokens, n_buckets;
+};
+// Entries below this mask: beside any other they have no weight, and where a row has nothing else, its logarithm of the sum would have no bits
+// left for S (a type's lowest value times log2 e is not even finite).  Such rows are rows without a key.
+constexpr float kRelMasked = -1e6f;
+__device__ __forceinline__ float rel_entry(float v, float mul) { return (v < kRelMasked ? __uint_as_float(0xff800000u) : v) * mul; }
+// Position of packed row i (< the packed rows) whose token is t; before: the token of the row before it (or t), start: its segment's first
+// row.  An error in d_status for a token out of range, or a segment with tokens of two images.
+template <typename Start>
+__device__ __forceinline__ int rel_position(int t, int before, int i, int N, int cols, int tokens, Start start, int32_t* d_status) {
+  if ((unsigned)t >= (unsigned)tokens) {
+    record_status(d_status, SPA_ERR_INVALID_ARG);
+    return 0;
+  }
+  const int n = t % N;
+  if (t / N != before / N && start() != i) record_status(d_status, SPA_ERR_INVALID_ARG);
+  return n / cols * (2 * cols - 1) + n % cols;
+}
+
 // A half of a row of the forward's output that is not finite: {row, head, half}, and the CTA's entry before it (numbers from 1 on; 0:
 // none), of which `last` in shared memory is the last.  The CTA that notes it down forms it again.
-__device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int row, int h, int half) {
-  const uint32_t at = atomicAdd(redo, 1u) + 1u;
+__device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int capacity, int row, int h, int half) {
+  const uint32_t at = 2u * ((uint32_t)h * capacity + row) + half + 1u;
   redo[2 * at - 1] = (uint32_t)row | (uint32_t)h << 20 | (uint32_t)half << 28;
   redo[2 * at] = atomicExch(last, at);
 }
@@ -186,7 +209,8 @@ int launch_attention_rel_bwd_short(const spa_params& p, const void* qkv, const v
                                    const int32_t* seg, int n_seg, const RelBwd& rel, void* dqkv, float* delta, int32_t* d_status,
                                    cudaStream_t st);
 int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
-                                float* lse, float* peak, int32_t* d_status, cudaStream_t st);
+                                float* lse, float* peak, const RelRaw* raw, int32_t* d_status, cudaStream_t st);
+bool attention_rel_fwd_prepares(const spa_params& p, int pitch);  // launch_attention_rel_fwd_tc with raw, and no preparation before it
 int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void* ao, const float* lse, const void* dao,
                                 const int32_t* seg, int n_seg, const RelView& view, const RelGrad& grad, void* dqkv, float* delta,
                                 int32_t* d_status, cudaStream_t st);

@@ -72,7 +72,10 @@ constexpr int kOnePerSm = 227 * 1024;
 // No more than a CTA per SM: it may take all of the SM's memory
 bool few_items(const spa_params& p) { return (long long)p.H * ((p.capacity + kQ - 1) / kQ) <= kNumSMs; }
 // Where the bias by relative position is read (attn_rel.cu): nowhere, in shared memory, in global memory
-enum RelTable { kNoRel = 0, kRelShared = 1, kRelGlobal = 2 };
+// kRelOwn: in shared memory, and the kernel prepares table and positions itself
+enum RelTable { kNoRel = 0, kRelShared = 1, kRelGlobal = 2, kRelOwn = 3 };
+constexpr int kOwnEntries = 3;  // of the table: a thread's, fetched together
+__host__ __device__ constexpr bool in_shared(int rel) { return rel == kRelShared || rel == kRelOwn; }
 
 template <int D, int kRel = kNoRel> struct FwdSmem {
   // Q, 2 x K, 2 x V.  Two CTAs stay below 196 KB of an SM: with 228 (a second Q tile) the kernels that run before and after
@@ -88,28 +91,39 @@ template <int D, int kRel = kNoRel> struct FwdSmem {
   static constexpr int kPos = kOrder + (int)sizeof(ItemOrder);
   static constexpr int kTable = kPos + (kRel != kNoRel ? 4 * 2 * kKV * 4 : 0);
   static constexpr int kBytes = kTable + 1024;  // and the alignment of the base
-  static constexpr int bytes(int pitch) { return kBytes + (kRel == kRelShared ? pitch * 4 : 0); }
+  static constexpr int bytes(int pitch) { return kBytes + (in_shared(kRel) ? pitch * 4 : 0); }
 };
 
+// Position of packed row i: prepared, or from its token
+template <int kRel> __device__ __forceinline__ int position_of(const RelView& rel, const RelRaw& raw, int Np, int i) {
+  if constexpr (kRel == kRelOwn) {
+    if (i >= Np) return 0;
+    const int t = ld_dep(raw.idx + i);
+    return rel_position(t, t, i, raw.N, raw.cols, raw.tokens, [] { return 0; }, nullptr);
+  } else {
+    return rel.pos[i];
+  }
+}
+
 // The rows that this CTA has noted down (see rel_fwd_note), from entry `at` on: a half of a row's output from the keys of its segment
-// alone, by a warp, the keys to its lanes.
+// alone, by a warp, the keys to its lanes.  table: the CTA's head's.
+template <int kRel>
 __device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, const int32_t* seg, int n_seg, int Np, int C, int d,
-                                           float scale_log2e, const int32_t* pos, const float* table, int pitch, int center,
-                                           const uint32_t* redo, uint32_t at) {
+                                           float scale_log2e, const RelView rel, const RelRaw raw, const float* table, uint32_t at) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = 0; at != 0u; ++i) {
-    const uint32_t what = redo[2 * at - 1];
-    at = redo[2 * at];
+    const uint32_t what = rel.redo[2 * at - 1];
+    at = rel.redo[2 * at];
     if (i % (kFwdThreads / 32) != warp) continue;
     const int row = what & 0xfffff, h = (what >> 20) & 0xff, first = ((what >> 28) & 1) * (d / 2);
     const RowSeg s = row_segment(seg, n_seg, Np, row);
     const __nv_bfloat16* q = qkv + (long long)row * 3 * C + h * d;
-    const float* bias = table + (long long)h * pitch + center + pos[row];
+    const float* bias = table + rel.center + position_of<kRel>(rel, raw, Np, row);
     auto logit = [&](int j) {
       const __nv_bfloat16* k = qkv + (long long)j * 3 * C + C + h * d;
       float v = 0.f;
       for (int e = 0; e < d; ++e) v = fmaf(__bfloat162float(q[e]), __bfloat162float(k[e]), v);
-      return fmaf(v, scale_log2e, bias[-pos[j]]);
+      return fmaf(v, scale_log2e, bias[-position_of<kRel>(rel, raw, Np, j)]);
     };
     float m = -CUDART_INF_F;
     for (int j = s.lo + lane; j < s.hi; j += 32) m = fmaxf(m, logit(j));
@@ -151,7 +165,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, int n_seg, int capacity,
                    int C, int H, float scale_log2e, __nv_bfloat16* __restrict__ ao, float* __restrict__ lse,
                    unsigned* counter, bool even_items, int32_t* d_status, const RelView rel, const __nv_bfloat16* qkv,
-                   float* __restrict__ peak) {
+                   float* __restrict__ peak, const RelRaw raw) {
   using HT = HeadTile<D>;
   using SM = FwdSmem<D, kRel>;
   constexpr int kTile = HT::kTileBytes;
@@ -212,6 +226,24 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   const int Np = packed_rows(seg, n_seg, capacity);
   const int row_tiles = (Np + kQ - 1) / kQ, n_items = row_tiles * H;
   if ((int)blockIdx.x >= n_items) return;
+  if constexpr (kRel == kRelOwn) {
+    const int h = (int)blockIdx.x % H;
+    for (int o = tid; o < rel.entries; o += kOwnEntries * kFwdThreads) {
+      int b[kOwnEntries];
+      float v[kOwnEntries];
+#pragma unroll
+      for (int u = 0; u < kOwnEntries; ++u) b[u] = o + u * kFwdThreads < rel.entries ? raw.bucket[o + u * kFwdThreads] : 0;
+#pragma unroll
+      for (int u = 0; u < kOwnEntries; ++u) {
+        const bool ok = (unsigned)b[u] < (unsigned)raw.n_buckets;
+        if (!ok) record_status(d_status, SPA_ERR_INVALID_ARG);
+        v[u] = ok ? __bfloat162float(static_cast<const __nv_bfloat16*>(raw.table)[(long long)b[u] * H + h]) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kOwnEntries; ++u)
+        if (o + u * kFwdThreads < rel.entries) reinterpret_cast<float*>(smem_al + SM::kTable)[o + u * kFwdThreads] = rel_entry(v[u], 1.4426950408889634f);
+    }
+  }
   if (warp == 0) ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
   // Items are drawn behind the whole row tiles that the CTAs start with; longest first where their lengths differ, where
   // they are few enough to be put in order, and where CTAs take 1.5 of them or more (below that, who ends first takes
@@ -475,19 +507,29 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       float m = -CUDART_INF_F, l = 0.f;  // m: the maximum the stored P and O refer to (may lag the true one by kRescaleGap)
       // With a bias: this thread's two of the tile's key positions (as distances in the table, in bytes, negative), its row's place
       // in the table
-      const int* key_pos = nullptr;
+      int key_row = 0;
       uint32_t bias_at = 0;
       const char* bias_g = nullptr;
       float top = -CUDART_INF_F;
       const uint32_t pos_q = smem_base + SM::kPos + quarter * 2 * kKV * 4;
       if constexpr (kRel != kNoRel) {
-        key_pos = rel.pos + ptx::lds_s32(item_slot(it) + 8) + 2 * (half * 32 + lane);
-        const int own = rel.pos[ptx::lds_s32(item_slot(it)) + rl], k0 = key_pos[0], k1 = key_pos[1];
+        key_row = ptx::lds_s32(item_slot(it) + 8) + 2 * (half * 32 + lane);
+        const int k0 = position_of<kRel>(rel, raw, Np, key_row), k1 = position_of<kRel>(rel, raw, Np, key_row + 1);
+        const int own_row = ptx::lds_s32(item_slot(it)) + rl;
+        int own = 0;
+        if constexpr (kRel == kRelOwn) {
+          if (own_row < Np) {
+            const int t = ld_dep(raw.idx + own_row), before = own_row > 0 ? ld_dep(raw.idx + own_row - 1) : t;
+            own = rel_position(t, before, own_row, raw.N, raw.cols, raw.tokens, [&] { return mine.lo; }, d_status);
+          }
+        } else {
+          own = rel.pos[own_row];
+        }
         ptx::sts_2s32(pos_q + (g & 1) * kKV * 4 + 8 * (half * 32 + lane), -4 * k0, -4 * k1);
         bias_at = 4 * (rel.center + own);
-        if constexpr (kRel == kRelShared) {
+        if constexpr (in_shared(kRel)) {
           bias_at += table_s;
-          if (it == 0) wait(bar_table, 0);
+          if (kRel == kRelShared && it == 0) wait(bar_table, 0);
         } else {
           bias_g = reinterpret_cast<const char*>(rel.bias + (long long)ptx::lds_s32(item_slot(it) + 4) * rel.pitch);
         }
@@ -496,8 +538,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       for (; left > 0; --left, ++g, lo -= kKV, hi -= kKV) {
         int k0 = 0, k1 = 0;
         if constexpr (kRel != kNoRel) {
-          key_pos += kKV;
-          if (left > 1) { k0 = key_pos[0]; k1 = key_pos[1]; }
+          key_row += kKV;
+          if (left > 1) { k0 = position_of<kRel>(rel, raw, Np, key_row); k1 = position_of<kRel>(rel, raw, Np, key_row + 1); }
         }
         // ---- S_t into registers: TMEM loads in flight together, one wait
         wait(bar_s, g & 1);
@@ -524,7 +566,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
                 float b[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                  b[u] = kRel == kRelShared ? ptx::lds_f32(bias_at + k[u]) : *reinterpret_cast<const float*>(bias_g + (bias_at + k[u]));
+                  b[u] = in_shared(kRel) ? ptx::lds_f32(bias_at + k[u]) : *reinterpret_cast<const float*>(bias_g + (bias_at + k[u]));
 #pragma unroll
                 for (int u = 0; u < 4; u += 2) {
                   uint32_t* v = s + c * 32 + j + u;
@@ -683,7 +725,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       }
       if constexpr (kRel != kNoRel) {
         // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, at the end
-        if (again) rel_fwd_note(rel.redo, reinterpret_cast<uint32_t*>(smem_al + SM::kBar + 216), row, h, half);
+        if (again) rel_fwd_note(rel.redo, reinterpret_cast<uint32_t*>(smem_al + SM::kBar + 216), capacity, row, h, half);
       }
       if (half == 0 && rl < rows) {
         lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
@@ -701,7 +743,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   }
   if constexpr (kRel != kNoRel) {
     const uint32_t at = (uint32_t)ptx::lds_s32(redo_first);
-    if (at != 0u) rel_fwd_again(qkv, ao, seg, n_seg, Np, C, D, scale_log2e, rel.pos, rel.bias, rel.pitch, rel.center, rel.redo, at);
+    const float* table = in_shared(kRel) ? reinterpret_cast<const float*>(smem_al + SM::kTable) : rel.bias + (long long)((int)blockIdx.x % H) * rel.pitch;
+    if (at != 0u) rel_fwd_again<kRel>(qkv, ao, seg, n_seg, Np, C, D, scale_log2e, rel, raw, table, at);
   }
 }
 
@@ -2314,14 +2357,14 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
 
 template <int D, int kRel>
 int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
-               float* peak, int32_t* d_status, cudaStream_t st) {
+               float* peak, const RelRaw& raw, int32_t* d_status, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_tmap_bf16_2d(&tm, qkv, 3ull * p.C, p.capacity, 6ull * p.C, D, 128, D * 2)) return SPA_ERR_UNSUPPORTED;
   auto kern = attn_fwd_tc_kernel<D, kRel>;
   const int smem = FwdSmem<D, kRel>::bytes(rel.pitch);
   static DeviceOnce attr;
   cudaError_t ea = attr.run([&] {
-    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRel == kRelShared ? kOnePerSm : smem);
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, in_shared(kRel) ? kOnePerSm : smem);
   });
   if (ea != cudaSuccess) { set_cuda_error(ea, "attn_fwd_tc_kernel"); return SPA_ERR_CUDA; }
   // a persistent grid: two CTAs per SM (at most 94 KB of shared memory, 256 TMEM columns each), never more than work items
@@ -2333,17 +2376,18 @@ int fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_s
   const bool even_items = (long long)p.capacity <= 512ll * (n_seg > 0 ? n_seg : 1);
   launch_pdl(kern, grid, kFwdThreads, smem, st, tm, seg, n_seg, p.capacity, p.C, p.H,
              softmax_scale_of(p) * 1.4426950408889634f, (__nv_bfloat16*)ao, lse, kRel == kNoRel && items > grid ? item_counter(ao) : nullptr,
-             even_items, d_status, rel, (const __nv_bfloat16*)qkv, peak);
+             even_items, d_status, rel, (const __nv_bfloat16*)qkv, peak, raw);
   SPA_CUDA_CHECK_LAUNCH("attn_fwd_tc_kernel");
   return SPA_OK;
 }
 
 template <int D>
 int rel_fwd_launch(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao, float* lse,
-                   float* peak, int32_t* d_status, cudaStream_t st) {
+                   float* peak, const RelRaw* raw, int32_t* d_status, cudaStream_t st) {
+  if (raw != nullptr) return fwd_launch<D, kRelOwn>(p, qkv, seg, n_seg, rel, ao, lse, peak, *raw, d_status, st);
   if (FwdSmem<D, kRelShared>::bytes(rel.pitch) <= (few_items(p) ? kOnePerSm : kTwoPerSm))
-    return fwd_launch<D, kRelShared>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
-  return fwd_launch<D, kRelGlobal>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
+    return fwd_launch<D, kRelShared>(p, qkv, seg, n_seg, rel, ao, lse, peak, RelRaw{}, d_status, st);
+  return fwd_launch<D, kRelGlobal>(p, qkv, seg, n_seg, rel, ao, lse, peak, RelRaw{}, d_status, st);
 }
 
 }  // namespace
@@ -2396,14 +2440,22 @@ int launch_attention_rel_bwd_tc(const spa_params& p, const void* qkv, const void
 
 int launch_attention_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, void* ao, float* lse,
                             int32_t* d_status, cudaStream_t st) {
-  return p.C / p.H == 64 ? fwd_launch<64, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, d_status, st)
-                         : fwd_launch<32, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, d_status, st);
+  return p.C / p.H == 64 ? fwd_launch<64, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, RelRaw{}, d_status, st)
+                         : fwd_launch<32, kNoRel>(p, qkv, seg, n_seg, RelView{}, ao, lse, nullptr, RelRaw{}, d_status, st);
+}
+
+// Few items and a small table: a launch less, and a thread has three entries of the table to look up.  Forward in a graph (in a loop), us, with the
+// preparation -> without: one image of 14 x 14 with half selected, 6 heads of 64, 8.6 -> 8.0 (14.3 -> 9.7), 8 of 12 x 14, 4 of 32, 11.6 -> 11.1; four
+// entries: 3 of 16 x 18, 8 of 32, 14.0 -> 14.1, 4 of 18 x 15, 2 of 32, 15.8 -> 16.6; eight: 2 of 24 x 24, 12 of 64, 25.2 -> 27.5.
+bool attention_rel_fwd_prepares(const spa_params& p, int pitch) {
+  const int smem = p.C / p.H == 64 ? FwdSmem<64, kRelOwn>::bytes(pitch) : FwdSmem<32, kRelOwn>::bytes(pitch);
+  return few_items(p) && pitch <= kOwnEntries * kFwdThreads && smem <= kOnePerSm;
 }
 
 int launch_attention_rel_fwd_tc(const spa_params& p, const void* qkv, const int32_t* seg, int n_seg, const RelView& rel, void* ao,
-                                float* lse, float* peak, int32_t* d_status, cudaStream_t st) {
-  return p.C / p.H == 64 ? rel_fwd_launch<64>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st)
-                         : rel_fwd_launch<32>(p, qkv, seg, n_seg, rel, ao, lse, peak, d_status, st);
+                                float* lse, float* peak, const RelRaw* raw, int32_t* d_status, cudaStream_t st) {
+  return p.C / p.H == 64 ? rel_fwd_launch<64>(p, qkv, seg, n_seg, rel, ao, lse, peak, raw, d_status, st)
+                         : rel_fwd_launch<32>(p, qkv, seg, n_seg, rel, ao, lse, peak, raw, d_status, st);
 }
 
 }  // namespace spa
