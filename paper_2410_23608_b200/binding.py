@@ -94,6 +94,9 @@ class SpaSandwich(C.Structure):
                 ("g_post", C.c_void_p), ("b_post", C.c_void_p), ("g_pre", C.c_void_p), ("b_pre", C.c_void_p)]
 
 
+_DTYPES = {torch.float32: SPA_F32, torch.bfloat16: SPA_BF16}
+
+
 def make_params(B, N, Cc, H, dtype, capacity=None, flags=0, tau=0.0, softmax_scale=0.0) -> SpaParams:
     dt = {"f32": SPA_F32, "bf16": SPA_BF16, torch.float32: SPA_F32, torch.bfloat16: SPA_BF16}.get(dtype, dtype)
     return SpaParams(B, N, Cc, H, dt, flags, capacity if capacity is not None else max(B * N, 1), tau, softmax_scale)
@@ -283,11 +286,19 @@ def rel_bias(rows, cols, bucket, table) -> SpaRelBias:
     """A spa_rel_bias from the device tensors bucket (int32 [(2 rows - 1) (2 cols - 1)]) and table ([n_buckets, H]), which it keeps."""
     if bucket.dtype != torch.int32 or bucket.numel() != (2 * rows - 1) * (2 * cols - 1):
         raise ValueError("bucket: int32, one for each of the (2 rows - 1) (2 cols - 1) offsets")
-    if table.dim() != 2:
-        raise ValueError("table: [n_buckets, H]")
+    if table.dim() != 2 or table.dtype not in _DTYPES:
+        raise ValueError("table: [n_buckets, H], float32 or bfloat16")
     r = SpaRelBias(int(rows), int(cols), int(table.shape[0]), _ptr(bucket), _ptr(table))
     r.tensors = (bucket, table)
+    r.of = (_DTYPES[table.dtype], int(table.shape[1]))
     return r
+
+
+def _check_rel(p, rel):
+    """The library sees an address: a table of another type, or of fewer heads, would be read as what it is not, and past its end."""
+    of = getattr(rel, "of", None)
+    if of is not None and of != (p.dtype, p.H):
+        raise ValueError("table: the problem's type, and a column for each of its heads")
 
 
 def spa_rel_workspace_bytes(p, rel) -> int:
@@ -295,6 +306,7 @@ def spa_rel_workspace_bytes(p, rel) -> int:
 
 
 def spa_packed_attention_rel_fwd(p, rel, qkv, seg_offsets, n_seg, idx, attn_out, lse, peak, workspace, d_status=None, stream=None):
+    _check_rel(p, rel)
     _check(lib().spa_packed_attention_rel_fwd(C.byref(p), C.byref(rel), _ptr(qkv), _ptr(seg_offsets), int(n_seg), _ptr(idx), _ptr(attn_out),
                                               _ptr(lse), _ptr(peak), _ptr(workspace), _ptr(d_status), _stream(stream)),
            "spa_packed_attention_rel_fwd")
@@ -302,6 +314,7 @@ def spa_packed_attention_rel_fwd(p, rel, qkv, seg_offsets, n_seg, idx, attn_out,
 
 def spa_packed_attention_rel_bwd(p, rel, qkv, attn_out, lse, peak, d_attn_out, seg_offsets, n_seg, idx, dqkv, dtable, workspace,
                                  d_status=None, stream=None):
+    _check_rel(p, rel)
     _check(lib().spa_packed_attention_rel_bwd(C.byref(p), C.byref(rel), _ptr(qkv), _ptr(attn_out), _ptr(lse), _ptr(peak), _ptr(d_attn_out),
                                               _ptr(seg_offsets), int(n_seg), _ptr(idx), _ptr(dqkv), _ptr(dtable), _ptr(workspace),
                                               _ptr(d_status), _stream(stream)), "spa_packed_attention_rel_bwd")
