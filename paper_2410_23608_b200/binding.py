@@ -430,10 +430,30 @@ def sandwich(kind="layer", gate_kind="none", gate=None, scale=None, g_post=None,
     tensors = (gate, scale, g_post, b_post, g_pre, b_pre)
     s = SpaSandwich(_NORM_KINDS.get(kind, kind), _GATE_KINDS.get(gate_kind, gate_kind), float(eps), *(_ptr(t) for t in tensors))
     s.tensors = tensors
+    gated = [gate] if s.gate_kind in (SPA_GATE_IMAGE, SPA_GATE_TOKEN) and gate is not None else []
+    types = {t.dtype for t in tensors[1:] if t is not None} | {t.dtype for t in gated}
+    sizes = {t.numel() for t in tensors[1:] if t is not None}
+    if len(types) > 1 or not types <= set(_DTYPES) or len(sizes) > 1:
+        raise ValueError("scale, g_post, b_post, g_pre, b_pre, a gate per image or token: one type, float32 or bfloat16; the five: one size")
+    s.of = (_DTYPES[types.pop()] if types else None, sizes.pop() if sizes else None, None if gate is None else gate.numel())
     return s
 
 
+def _check_sandwich(p, s):
+    """The library sees addresses: parameters of another type or size would be read as what they are not, and past their ends."""
+    of = getattr(s, "of", None)
+    if of is None:
+        return
+    dtype, C_, gate = of
+    if (dtype is not None and dtype != p.dtype) or (C_ is not None and C_ != p.C):
+        raise ValueError("scale, g_post, b_post, g_pre, b_pre: C values each of the problem's type")
+    k = s.gate_kind
+    if gate is not None and k and gate < (p.B * p.N if k == SPA_GATE_SCORE else p.B * p.C if k == SPA_GATE_IMAGE else p.B * p.N * p.C):
+        raise ValueError("gate: no fewer than B * N scores, B * C values of a gate per image, or B * N * C of one per token")
+
+
 def spa_sandwich_norm(p, s, x, z, z_row, y, n, stats=None, stream=None):
+    _check_sandwich(p, s)
     _check(lib().spa_sandwich_norm(C.byref(p), C.byref(s), _ptr(x), _ptr(z), _ptr(z_row), _ptr(y), _ptr(n), _ptr(stats), _stream(stream)),
            "spa_sandwich_norm")
 
@@ -444,6 +464,7 @@ def spa_sandwich_workspace_bytes(p, s) -> int:
 
 def spa_sandwich_norm_bwd(p, s, dn, dy, y, z, z_row, stats, dx, dz, dgate=None, dscale=None, dg_post=None, db_post=None, dg_pre=None,
                           db_pre=None, workspace=None, stream=None):
+    _check_sandwich(p, s)
     _check(lib().spa_sandwich_norm_bwd(C.byref(p), C.byref(s), _ptr(dn), _ptr(dy), _ptr(y), _ptr(z), _ptr(z_row), _ptr(stats), _ptr(dx),
                                        _ptr(dz), _ptr(dgate), _ptr(dscale), _ptr(dg_post), _ptr(db_post), _ptr(dg_pre), _ptr(db_pre),
                                        _ptr(workspace), _stream(stream)), "spa_sandwich_norm_bwd")

@@ -35,3 +35,48 @@ def test_table_of_another_type_or_width(lib, problem, table, H):
 def test_table_of_no_type_of_the_library(lib, dtype):
     with pytest.raises(ValueError):
         lib.rel_bias(3, 5, torch.zeros(45, dtype=torch.int32), torch.zeros(7, 2, dtype=dtype))
+
+
+def _sandwich_calls(lib, p, s):
+    t = torch.zeros(4096)
+    return (lambda: lib.spa_sandwich_norm(p, s, None, t, None, t, t, t),                    # x = None: refused by the library, if not before
+            lambda: lib.spa_sandwich_norm_bwd(p, s, t, t, None, t, None, t, t, t, workspace=t))
+
+
+NAMES = ("scale", "g_post", "b_post", "g_pre", "b_pre")
+
+
+@pytest.mark.parametrize("problem", ["f32", "bf16"])
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("dtype,size", [(torch.float32, 64), (torch.bfloat16, 64), (torch.float32, 56), (torch.bfloat16, 72)])
+def test_parameters_of_another_type_or_size(lib, problem, name, dtype, size):
+    p = lib.make_params(2, 15, 64, 1, problem)
+    s = lib.sandwich("layer", "none", **{name: torch.zeros(size, dtype=dtype)})
+    right = size == 64 and (dtype == torch.float32) == (problem == "f32")
+    for call in _sandwich_calls(lib, p, s):
+        with pytest.raises(lib.SpaError if right else ValueError):
+            call()
+
+
+@pytest.mark.parametrize("problem", ["f32", "bf16"])
+@pytest.mark.parametrize("kind,right", [("score", 30), ("image", 128), ("token", 1920)])
+@pytest.mark.parametrize("size", [24, 32, 120, 128, 1912, 1920])   # a buffer for larger batches may be given
+def test_gates_of_another_type_or_size(lib, problem, kind, right, size):
+    p = lib.make_params(2, 15, 64, 1, problem)
+    for dtype in (torch.float32, torch.bfloat16):
+        if kind == "score" and dtype == torch.bfloat16:
+            continue                                        # refused when it is made
+        s = lib.sandwich("rms", kind, gate=torch.zeros(size, dtype=dtype))
+        ok = size >= right and (kind == "score" or (dtype == torch.float32) == (problem == "f32"))
+        for call in _sandwich_calls(lib, p, s):
+            with pytest.raises(lib.SpaError if ok else ValueError):
+                call()
+
+
+def test_parameters_that_differ_among_themselves(lib):
+    f, b = torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)
+    for kw in (dict(scale=f, g_pre=b), dict(scale=f, g_pre=f[:32]), dict(scale=b, gate=f, gate_kind="image"), dict(b_pre=f.half()),
+               dict(gate=f.half(), gate_kind="token")):
+        with pytest.raises(ValueError):
+            lib.sandwich("layer", **kw)
+    lib.sandwich("layer", "score", gate=f, scale=b)          # scores are fp32 beside parameters of any type
