@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
   for (int h = warp; h < g.H; h += 8) {
     const float b = rel_head_bound(g, h);
     const bool ok = b < __uint_as_float(0x7f800000u) && ld_dep(g.bad + h) == 0;
-    if (lane == 0) unit[h] = ok ? __uint_as_float((uint32_t)(127 - kRelBits + rel_exponent(b)) << 23) : __uint_as_float(0x7fc00000u);
+    if (lane == 0) unit[h] = ok ? rel_power(rel_exponent(b) - g.bits) : __uint_as_float(0x7fc00000u);
   }
   __syncthreads();
   const int tid = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
@@ -339,6 +339,7 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   g.bad = (int32_t*)(ws + l.bad);
   g.redo = (uint32_t*)(ws + l.redo);
   g.H = p.H;
+  g.bits = rel_bits(p.capacity);
   g.most_redo = 4u * p.H * p.capacity;
   rc = tc ? launch_attention_rel_bwd_tc(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, (float*)(ws + l.delta), d_status, st)
           : launch_attention_rel_bwd_simt(p, qkv, ao, lse, dao, seg, n_seg, view(l, ws), g, dqkv, st);

@@ -56,7 +56,7 @@ __device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int
 
 constexpr int kRelBlocks = kNumSMs;  // CTAs of the kernel that prepares a call, each with its own maxima
 struct RelGrad {
-  // [H][places] sums of dS times 2^(kRelBits - exponent of the head's bound): a place for each bucket, or, where they are few
+  // [H][places] sums of dS times 2^(bits - exponent of the head's bound): a place for each bucket, or, where they are few
   // (rel_few_buckets), one for each offset, and rel_fold_kernel behind the attention
   unsigned long long* acc;
   const int32_t* place;  // [entries]: the buckets, or the offsets themselves (a NULL for these, and a branch, made the dQ pass 3 % slower)
@@ -65,6 +65,7 @@ struct RelGrad {
   int32_t* bad;             // [H] a row's statistics are not finite
   uint32_t* redo;           // [1 + 4 H capacity] how many, and which parts of rows are to be formed again
   int places, H;
+  int bits;                 // see rel_bits
   uint32_t most_redo;       // 4 H capacity
 };
 
@@ -75,15 +76,22 @@ __device__ __forceinline__ void rel_redo(const RelGrad& g, bool keys, int half, 
   if (at < g.most_redo) g.redo[1 + at] = (uint32_t)row | (uint32_t)h << 20 | (keys ? 1u : 0u) << 28 | (uint32_t)half << 29;
 }
 
-// Bits of the head's bound.  A bin has at most one pair per query, 2^20 in all, and the bound is taken up to a power of two.
-constexpr int kRelBits = 42;
+// Bits of the head's bound in the sums: as many as 64 hold.  The pairs of a query in a bin have dS of no more than the bound together (their P sum
+// to one), the bound is taken up to a power of two, and D from a rounded O makes it 2^-8 more: capacity 2^bits < 2^62 1.01.  (A unit of 2^46 is what a
+// float's exponent holds beside the least bound.)
+constexpr int kRelMostBits = 46;
+inline int rel_bits(int capacity) {
+  int log2_rows = 0;
+  while ((1 << log2_rows) < capacity) ++log2_rows;
+  return 62 - log2_rows < kRelMostBits ? 62 - log2_rows : kRelMostBits;
+}
 
 // Exponent e of a bound b < 2^e; zero and values too small for the scale's exponent count as the smallest.
 __device__ __forceinline__ int rel_exponent(float b) {
   const int e = (int)((__float_as_uint(b) >> 23) & 0xffu) - 126;
   return e < -80 ? -80 : e;
 }
-__device__ __forceinline__ float rel_scale(int e) { return __uint_as_float((uint32_t)(127 + kRelBits - e) << 23); }
+__device__ __forceinline__ float rel_power(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }
 
 // 2 max |dO| max |v| of a head, and max |v|, by a converged warp.  Maxima of bit patterns: a NaN is larger than every number.  Squares that
 // underflow count as the smallest normal number: a bound may be too large, not too small.
@@ -136,18 +144,35 @@ struct RelBwd {
   RelGrad grad;
   bool shared_bins;
 };
-// The bins of an item are two words: a pair adds the low ten bits of its dS, a number below 2^kRelItemBits in units of the scale, to one and
-// the others to the other.  A bin has at most one pair of each of the item's 128 query rows, since a token is in its segment once:
-// neither overflows.  (One word holds 23 bits of a pair, and the bound is a thousand times what a pair has on average: the gradient of
-// 32 images of 24 x 24 tokens was off by 3.6e-5.)
-constexpr int kRelItemBits = 30, kRelLow = 10;
-__device__ __forceinline__ void rel_bin(uint32_t at, uint32_t pitch_bytes, float scaled) {
-  const int v = __float2int_rn(scaled);
-  ptx::red_add_s32(at, v & ((1 << kRelLow) - 1));
-  ptx::red_add_s32(at + pitch_bytes, v >> kRelLow);
+// An item's pairs are multiples of 2^-44 of the item's bound: 21 bits in front of a point, to which a pair is rounded by the addition of a number
+// whose unit that is, and the rest, which is exact, times 2^23 in the same way (|rest| <= 1/2).  As pairs of fp32, without a conversion.  The two
+// parts go to two words of a bin, which has at most one pair of each of the item's 128 query rows, since a token is in its segment
+// once: 2^21 (1.01 of it, see rel_bits) and 2^22 times 2^7 overflow neither.  (30 bits of a pair, by a conversion and ten bits of the integer to one
+// word: one row of V 1 000 times as large as the others, in another image, took the gradient's error from below 2e-7 to up to 5e-4, since the
+// bound that all rows of a head share was 1 000 times what they needed.  32 images of 24 x 24, 12 heads of 64, backward 197 -> 202 us.
+// One word of 23 bits: an error of 3.6e-5 without any such row.)
+constexpr int kRelHigh = 21, kRelLow = 23, kRelItemBits = kRelHigh + kRelLow;
+constexpr uint32_t kRelUnits = 0x4b400000u;  // 1.5 * 2^23: adding it rounds |x| < 2^22 to an integer, in the low bits
+__device__ __forceinline__ float rel_item_scale(int bound_exp) { return rel_power(kRelHigh - bound_exp); }
+// Units of an item's scale to those of the head's: a shift to the left
+__device__ __forceinline__ int rel_item_shift(const RelGrad& g, int bound_exp, int head_exp) { return g.bits - head_exp - (kRelItemBits - bound_exp); }
+__device__ __forceinline__ void rel_fixed(uint64_t d, float scale, uint32_t* hi, uint32_t* lo) {  // of two pairs
+  const uint64_t s = ptx::pair(scale, scale), units = ptx::pair(kRelUnits, kRelUnits);
+  const uint64_t t = ptx::fma2(d, s, units);
+  const uint64_t rest = ptx::fma2(d, s, ptx::fma2(t, ptx::pair(-1.f, -1.f), units));
+  const uint64_t u = ptx::fma2(rest, ptx::pair((float)(1 << kRelLow), (float)(1 << kRelLow)), units);
+  ptx::unpair(t, hi[0], hi[1]);
+  ptx::unpair(u, lo[0], lo[1]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { hi[i] -= kRelUnits; lo[i] -= kRelUnits; }
 }
-// The fp32-FMA kernels: 42 bits of a pair in three words, 14 bits to each of the lower two; 32 query rows
-constexpr int kRelThird = 14;
+__device__ __forceinline__ void rel_bin(uint32_t at, uint32_t pitch_bytes, uint32_t hi, uint32_t lo) {
+  ptx::red_add_s32(at, (int)lo);
+  ptx::red_add_s32(at + pitch_bytes, (int)hi);
+}
+__device__ __forceinline__ long long rel_joined(int hi, int lo) { return ((long long)hi << kRelLow) + lo; }
+// The fp32-FMA kernels: up to 46 bits of a pair in three words, 16 bits to each of the lower two; 32 query rows
+constexpr int kRelThird = 16;
 __device__ __forceinline__ void rel_bin3(int* bin, int pitch, long long v) {
   atomicAdd(bin, (int)v & ((1 << kRelThird) - 1));
   atomicAdd(bin + pitch, (int)(v >> kRelThird) & ((1 << kRelThird) - 1));
@@ -157,9 +182,11 @@ template <int kThreads> __device__ __forceinline__ void rel_flush3(const RelGrad
   for (int i = tid; i < entries; i += kThreads)
     rel_add(g, h, i, ((long long)bins[2 * pitch + i] << 2 * kRelThird) + ((long long)bins[pitch + i] << kRelThird) + bins[i]);
 }
-// A sum in units of an item's scale as one in units of the head's
+// A sum in units of an item's scale as one in units of the head's, to nearest (|v| <= 2^52)
 __device__ __forceinline__ long long rel_shifted(long long v, int shift) {
-  return shift >= 0 ? v << shift : v >> (shift > -63 ? -shift : 63);
+  if (shift >= 0) return v << shift;
+  const int n = shift > -60 ? -shift : 60;
+  return (v + (1ll << (n - 1))) >> n;
 }
 
 // Positions of a tile's columns from shared memory, four at a time, and where registers allow (kAhead) a step before they are used: the
@@ -191,7 +218,7 @@ __device__ __forceinline__ void rel_flush(const RelBwd& rel, const int* bins, in
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int at = i + u * kThreads;
-      v[u] = at < rel.view.entries ? ((long long)bins[rel.view.pitch + at] << kRelLow) + bins[at] : 0;
+      v[u] = at < rel.view.entries ? rel_joined(bins[rel.view.pitch + at], bins[at]) : 0;
       b[u] = v[u] != 0 ? rel.grad.place[at] : -1;
     }
 #pragma unroll

@@ -191,8 +191,8 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
         __syncwarp();
       }
       const int bound_exp = rel_exponent(__uint_as_float(*reinterpret_cast<volatile uint32_t*>(tile_bound)));
-      const float bin_scale = __uint_as_float((uint32_t)(127 + kRelItemBits - bound_exp) << 23);
-      const int bin_shift = kRelBits - head_exp - (kRelItemBits - bound_exp);
+      const float bin_scale = rel_item_scale(bound_exp);
+      const int bin_shift = rel_item_shift(rel.grad, bound_exp, head_exp);
       const uint32_t bias_at = 4 * (rel.view.center + own_pos);
       wait(bar_s, parity);
       ptx::tc_fence_after_sync();
@@ -236,7 +236,6 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
-            const uint64_t bin2 = ptx::pair(bin_scale, bin_scale);
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
               pk_p[j >> 1] = ptx::bf16_pair(__uint_as_float(rs[j]), __uint_as_float(rs[j + 1]));
@@ -244,7 +243,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
               float d0, d1;
               ptx::unpair(d, d0, d1);
               pk_ds[part][j >> 1] = ptx::bf16_pair(d0, d1);
-              ptx::unpair(ptx::mul2(d, bin2), rp[j], rp[j + 1]);
+              rel_fixed(d, bin_scale, rs + j, rp + j);
             }
             // the table's gradient: a pair's bin is where its bias came from
             RelKeys<> again(pos_at);
@@ -253,7 +252,7 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
               int k[4];
               again.next(j, 32, k);
 #pragma unroll
-              for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rp[j + u]));
+              for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, rs[j + u], rp[j + u]);
             }
           }
           __syncwarp();
@@ -572,8 +571,8 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
         __syncwarp();
       }
       const int bound_exp = rel_exponent(__uint_as_float(*reinterpret_cast<volatile uint32_t*>(tile_bound)));
-      const float bin_scale = __uint_as_float((uint32_t)(127 + kRelItemBits - bound_exp) << 23);
-      const int bin_shift = kRelBits - head_exp - (kRelItemBits - bound_exp);
+      const float bin_scale = rel_item_scale(bound_exp);
+      const int bin_shift = rel_item_shift(rel.grad, bound_exp, head_exp);
       const uint32_t bias_at = 4 * (rel.view.center + own_pos);
       wait(bar_s, parity);
       ptx::tc_fence_after_sync();
@@ -614,7 +613,6 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
           }
 #pragma unroll
           for (int j = 0; j < 16; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
-          const uint64_t bin2 = ptx::pair(bin_scale, bin_scale);
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
             pk_p[j >> 1] = ptx::bf16_pair(__uint_as_float(rs[j]), __uint_as_float(rs[j + 1]));
@@ -622,7 +620,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
             float d0, d1;
             ptx::unpair(d, d0, d1);
             pk_ds[part * 8 + (j >> 1)] = ptx::bf16_pair(d0, d1);
-            ptx::unpair(ptx::mul2(d, bin2), rp[j], rp[j + 1]);
+            rel_fixed(d, bin_scale, rs + j, rp + j);
           }
           // the table's gradient: a pair's bin is where its bias came from
           RelKeys<> again(pos_at);
@@ -631,7 +629,7 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
             int k[4];
             again.next(j, 16, k);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rp[j + u]));
+            for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, rs[j + u], rp[j + u]);
           }
         }
         __syncwarp();

@@ -393,7 +393,7 @@ attn_bwd_simt_kernel(const T* qkv, const T* ao, const float* lse,
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i0 + ty + kTY * i < Np) own_pos[i] = rel.pos[i0 + ty + kTY * i];
-    if (dq) table_scale = rel_scale(rel_exponent(rel_head_bound(grad, h)));  // every warp takes it by itself
+    if (dq) table_scale = rel_power(grad.bits - rel_exponent(rel_head_bound(grad, h)));  // every warp takes it by itself
   }
   if (dq) {
     // lane tx < 4 fetches row ty + 8 tx, the others take it from there

@@ -1247,11 +1247,12 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
         if (lane == 0) atomicMax(item_bound, most);
         ptx::named_barrier(1, kBwdMath);
         const int e = rel_exponent(__uint_as_float(*reinterpret_cast<volatile uint32_t*>(item_bound)));
-        bin_scale = __uint_as_float((uint32_t)(127 + kRelItemBits - e) << 23);
-        bin_shift = kRelBits - head_exp - (kRelItemBits - e);
+        bin_scale = rel_item_scale(e);
+        bin_shift = rel_item_shift(rel.grad, e, head_exp);
         if (tid == 0) range[0] = bin_shift;  // everyone has read its own copy: o_lo
       } else {
-        bin_scale = rel_scale(head_exp);
+        bin_scale = rel_item_scale(head_exp);
+        bin_shift = rel_item_shift(rel.grad, head_exp, head_exp);
       }
     }
 
@@ -1323,28 +1324,32 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
           }
 #pragma unroll
           for (int j = 0; j < kPc; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
-#pragma unroll
-          for (int j = 0; j < kPc; j += 2) {
+auto ds_of = [&](int j) {
             float d0, d1;
             const uint64_t d = ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1]));
             ptx::unpair(d, d0, d1);
             pk_ds[j >> 1] = ptx::bf16_pair(d0, d1);
-            if (kRel != kNoRel) ptx::unpair(ptx::mul2(d, ptx::pair(bin_scale, bin_scale)), rs[j], rs[j + 1]);
-          }
-          if constexpr (kRel != kNoRel) {  // the table's gradient: a pair's bin is where its bias came from
+            return d;
+          };
+          if constexpr (kRel == kNoRel) {
+#pragma unroll
+            for (int j = 0; j < kPc; j += 2) ds_of(j);
+          } else {  // the table's gradient: a pair's bin is where its bias came from
             RelKeys<!kDQ> keys(pos_at);
 #pragma unroll
             for (int j = 0; j < kPc; j += 4) {
               int k[4];
               keys.next(j, kPc, k);
+              uint32_t hi[4], lo[4];
+#pragma unroll
+              for (int u = 0; u < 4; u += 2) rel_fixed(ds_of(j + u), bin_scale, hi + u, lo + u);
               if (rel.shared_bins) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                  rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, __uint_as_float(rs[j + u]));
+                for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, hi[u], lo[u]);
               } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                  rel_add(rel.grad, h, (int)(bias_at + k[u]) >> 2, __float2ll_rn(__uint_as_float(rs[j + u])));
+                  rel_add(rel.grad, h, (int)(bias_at + k[u]) >> 2, rel_shifted(rel_joined((int)hi[u], (int)lo[u]), bin_shift));
               }
             }
           }
