@@ -224,7 +224,7 @@ int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, c
  *   dtable[b][h] = sum of dS_ij over all pairs of all segments whose bucket is b     (float[n_buckets][H] out).
  * Bitwise reproducible: dS is summed in integers, as multiples of powers of two that bounds on its size give.  With the largest norm |v| of
  * the head's rows of V and p_i a row's largest probability (peak, of the same forward call; 1 without it, NULL), each dS is rounded by at
- * most 2^-44 of 2 p_i |d_attn_out_i| |v|, the largest of its 128 query rows, and what such 128 rows have in a bucket by 2^-b of
+ * most 2^-43 of 2 p_i |d_attn_out_i| |v|, the largest of its 128 query rows, and what such 128 rows have in a bucket by 2^-b of
  * 2 |d_attn_out_i| |v|, the largest of the head; b = 62 - log2(capacity), rounded down, at least 42 and at most 46.  fp32 problems and
  * SPA_FLAG_SIMT_ONLY: each dS by 2^-b of the head's.  No norm of a row of V or d_attn_out counts as less than 2^-63.  Where a value of V, K or d_attn_out, the square of a row's norm, or a row's lse or D is
  * not finite, the whole head's column of dtable may be NaN.  dqkv has infinities and NaN of a segment in that segment's rows only

@@ -144,27 +144,26 @@ struct RelBwd {
   RelGrad grad;
   bool shared_bins;
 };
-// An item's pairs are multiples of 2^-44 of the item's bound: 21 bits in front of a point, to which a pair is rounded by the addition of a number
-// whose unit that is, and the rest, which is exact, times 2^23 in the same way (|rest| <= 1/2).  As pairs of fp32, without a conversion.  The two
-// parts go to two words of a bin, which has at most one pair of each of the item's 128 query rows, since a token is in its segment
-// once: 2^21 (1.01 of it, see rel_bits) and 2^22 times 2^7 overflow neither.  (30 bits of a pair, by a conversion and ten bits of the integer to one
-// word: one row of V 1 000 times as large as the others, in another image, took the gradient's error from below 2e-7 to up to 5e-4, since the
-// bound that all rows of a head share was 1 000 times what they needed.  32 images of 24 x 24, 12 heads of 64, backward 197 -> 202 us.
-// One word of 23 bits: an error of 3.6e-5 without any such row.)
-constexpr int kRelHigh = 21, kRelLow = 23, kRelItemBits = kRelHigh + kRelLow;
+// An item's pairs are multiples of 2^-43 of the item's bound: 21 bits in front of a point, to which a pair is rounded by the addition of a number
+// whose unit that is, and the rest, which the next fma has exactly (|rest| <= 1/2), to 2^-22 by the addition of 3.  As pairs of fp32, without a
+// conversion.  The two parts go to two words of a bin, which has at most one pair of each of the item's 128 query rows, since a token is in its
+// segment once: 2^21 (1.01 of it, see rel_bits) and 2^21 times 2^7 overflow neither.  (30 bits of a pair, by a conversion and ten bits of the
+// integer to one word: one row of V 1 000 times as large as the others, in another image, took the gradient's error from below 2e-7 to up to
+// 5e-4, since the bound that all rows of a head share was 1 000 times what they needed.  32 images of 24 x 24, 12 heads of 64, backward
+// 192 -> 190 us, with the pairs' way to their bins moved behind the announcement of dS.  One word of 23 bits: an error of 3.6e-5 without any such row.)
+constexpr int kRelHigh = 21, kRelLow = 22, kRelItemBits = kRelHigh + kRelLow;
 constexpr uint32_t kRelUnits = 0x4b400000u;  // 1.5 * 2^23: adding it rounds |x| < 2^22 to an integer, in the low bits
+constexpr uint32_t kRelRest = 0x40400000u;   // 3, to whose side |x| <= 1/2 is rounded to 2^-22
 __device__ __forceinline__ float rel_item_scale(int bound_exp) { return rel_power(kRelHigh - bound_exp); }
 // Units of an item's scale to those of the head's: a shift to the left
 __device__ __forceinline__ int rel_item_shift(const RelGrad& g, int bound_exp, int head_exp) { return g.bits - head_exp - (kRelItemBits - bound_exp); }
 __device__ __forceinline__ void rel_fixed(uint64_t d, float scale, uint32_t* hi, uint32_t* lo) {  // of two pairs
-  const uint64_t s = ptx::pair(scale, scale), units = ptx::pair(kRelUnits, kRelUnits);
-  const uint64_t t = ptx::fma2(d, s, units);
-  const uint64_t rest = ptx::fma2(d, s, ptx::fma2(t, ptx::pair(-1.f, -1.f), units));
-  const uint64_t u = ptx::fma2(rest, ptx::pair((float)(1 << kRelLow), (float)(1 << kRelLow)), units);
+  const uint64_t s = ptx::pair(scale, scale), t = ptx::fma2(d, s, ptx::pair(kRelUnits, kRelUnits));
+  const uint64_t u = ptx::fma2(d, s, ptx::fma2(t, ptx::pair(-1.f, -1.f), ptx::pair(kRelUnits + 3, kRelUnits + 3)));  // 3 - hi, exact
   ptx::unpair(t, hi[0], hi[1]);
   ptx::unpair(u, lo[0], lo[1]);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) { hi[i] -= kRelUnits; lo[i] -= kRelUnits; }
+  for (int i = 0; i < 2; ++i) { hi[i] -= kRelUnits; lo[i] -= kRelRest; }
 }
 __device__ __forceinline__ void rel_bin(uint32_t at, uint32_t pitch_bytes, uint32_t hi, uint32_t lo) {
   ptx::red_add_s32(at, (int)lo);

@@ -236,23 +236,24 @@ rel_bwd_short_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_co
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              pk_p[j >> 1] = ptx::bf16_pair(__uint_as_float(rs[j]), __uint_as_float(rs[j + 1]));
-              const uint64_t d = ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1]));
-              float d0, d1;
-              ptx::unpair(d, d0, d1);
-              pk_ds[part][j >> 1] = ptx::bf16_pair(d0, d1);
-              rel_fixed(d, bin_scale, rs + j, rp + j);
-            }
             // the table's gradient: a pair's bin is where its bias came from
             RelKeys<> again(pos_at);
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
               int k[4];
               again.next(j, 32, k);
+              uint32_t hi[4], lo[4];
 #pragma unroll
-              for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, rs[j + u], rp[j + u]);
+              for (int u = j; u < j + 4; u += 2) {
+                pk_p[u >> 1] = ptx::bf16_pair(__uint_as_float(rs[u]), __uint_as_float(rs[u + 1]));
+                const uint64_t d = ptx::mul2(ptx::pair(rs[u], rs[u + 1]), ptx::pair(rp[u], rp[u + 1]));
+                float d0, d1;
+                ptx::unpair(d, d0, d1);
+                pk_ds[part][u >> 1] = ptx::bf16_pair(d0, d1);
+                rel_fixed(d, bin_scale, hi + u - j, lo + u - j);
+              }
+#pragma unroll
+              for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, hi[u], lo[u]);
             }
           }
           __syncwarp();
@@ -613,23 +614,24 @@ rel_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_con
           }
 #pragma unroll
           for (int j = 0; j < 16; ++j) rs[j] = __float_as_uint(ptx::ex2_approx(__uint_as_float(rs[j])));
-#pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            pk_p[j >> 1] = ptx::bf16_pair(__uint_as_float(rs[j]), __uint_as_float(rs[j + 1]));
-            const uint64_t d = ptx::mul2(ptx::pair(rs[j], rs[j + 1]), ptx::pair(rp[j], rp[j + 1]));
-            float d0, d1;
-            ptx::unpair(d, d0, d1);
-            pk_ds[part * 8 + (j >> 1)] = ptx::bf16_pair(d0, d1);
-            rel_fixed(d, bin_scale, rs + j, rp + j);
-          }
           // the table's gradient: a pair's bin is where its bias came from
           RelKeys<> again(pos_at);
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
             int k[4];
             again.next(j, 16, k);
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, rs[j + u], rp[j + u]);
+            for (int u = j; u < j + 4; u += 2) {
+              pk_p[u >> 1] = ptx::bf16_pair(__uint_as_float(rs[u]), __uint_as_float(rs[u + 1]));
+              const uint64_t d = ptx::mul2(ptx::pair(rs[u], rs[u + 1]), ptx::pair(rp[u], rp[u + 1]));
+              float d0, d1;
+              ptx::unpair(d, d0, d1);
+              pk_ds[part * 8 + (u >> 1)] = ptx::bf16_pair(d0, d1);
+              rel_fixed(d, bin_scale, hi + u - j, lo + u - j);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) rel_bin(bins_s + bias_at + k[u], rel.view.pitch * 4, hi[u], lo[u]);
           }
         }
         __syncwarp();

@@ -4,8 +4,9 @@ above the others makes the unit coarse for everyone.  What is left has to be as 
 The second image has all of its tokens, the first those of even rows: offsets of an odd number of rows are the second image's
 alone.  Its values, and what the kernels compute of them, are the same whatever the first image holds, so a difference between two calls
 in these buckets comes from the sums:
-  each of them  a pair is rounded to a unit of 2^-44 (fp32-FMA kernels: 2^-42 or finer) of a power of two of at most twice the bound
-          2 max |dO| max |v|, and its item's sum to one of 2^-42 or finer: half a unit each, 2^-44 + 2^-42 of the bound a pair, in both calls.
+  each of them  a pair is rounded to a unit of 2^-43 (fp32-FMA kernels: 2^-42 or finer) of a power of two of at most twice the bound
+          2 max |dO| max |v|, and its item's sum, with up to 2^16 rows, to one of 2^-46: half a unit each, 2^-43 + 2^-46 < 2^-44 + 2^-42 of the bound a
+          pair, in both calls.
   together  as good as fp32: 4 u = 2^-22 of the root mean square, of which 2 u are the roundings of the two results.  Half a unit for a
           thousand-fold V is 2^-46 2^10 of what the rows themselves need, which is 2^10 to 2^12 of a pair: 2^-24 of a pair, and of sums of many less.
 (As multiples of 2^-30 of the bound they were off by 2^-31 of it a pair: up to 5e-4 of the root mean square.)
