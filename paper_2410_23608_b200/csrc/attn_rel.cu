@@ -123,45 +123,29 @@ struct Redo {
   const __nv_bfloat16 *qkv, *dao;
   const float *lse, *delta;
   __nv_bfloat16* dqkv;
-  int C, d;
+  int C;
   float scale;
 };
-__device__ void redo_row(const Redo& r, const int32_t* seg, int n_seg, int capacity, int Np, uint32_t what) {
-  const int row = what & 0xfffff, h = (what >> 20) & 0xff, half = (what >> 29) & 1, lane = threadIdx.x & 31, n = r.d / 2;
+template <int D> __device__ void redo_row(const Redo& r, const int32_t* seg, int n_seg, int capacity, int Np, uint32_t what) {
+  const int row = what & 0xfffff, h = (what >> 20) & 0xff, e0 = ((what >> 29) & 1) * (D / 2), lane = threadIdx.x & 31;
   const bool keys = (what >> 28) & 1;
   const long long ld = 3LL * r.C;
-  const int col = h * r.d;
+  const int col = h * D;
   const RowSeg s = row_segment(seg, n_seg, Np, row);
-  const float* bias = r.view.bias + (long long)h * r.view.pitch + r.view.center;
-  for (int e0 = half * n; e0 < half * n + n; e0 += 8) {
-    float acc1[8] = {}, acc2[8] = {};
-    for (int k = s.lo + lane; k < s.hi; k += 32) {
-      const int q = keys ? k : row, j = keys ? row : k;
-      const __nv_bfloat16 *Q = r.qkv + q * ld + col, *K = r.qkv + j * ld + r.C + col, *dO = r.dao + (long long)q * r.C + col;
-      float dot = 0.f, dp = 0.f;
-      for (int e = 0; e < r.d; ++e) {
-        dot = fmaf(__bfloat162float(Q[e]), __bfloat162float(K[e]), dot);
-        dp = fmaf(__bfloat162float(dO[e]), __bfloat162float(K[r.C + e]), dp);
-      }
-      const float l = r.lse[(long long)h * capacity + q];
-      const float p = l == -CUDART_INF_F ? 0.f : exp2f(fmaf(dot, r.scale * kLog2e, bias[r.view.pos[q] - r.view.pos[j]]) - l * kLog2e);
-      const float ds = p * (dp - r.delta[(long long)h * capacity + q]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        acc1[e] = fmaf(ds, __bfloat162float((keys ? Q : K)[e0 + e]), acc1[e]);
-        acc2[e] = fmaf(p, __bfloat162float(dO[e0 + e]), acc2[e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      acc1[e] = warp_sum(acc1[e]) * r.scale;
-      acc2[e] = warp_sum(acc2[e]);
-    }
-    if (lane == 0) {
-      *reinterpret_cast<uint4*>(r.dqkv + row * ld + (keys ? r.C : 0) + col + e0) = Vec16<__nv_bfloat16>::from_float(acc1);
-      if (keys) *reinterpret_cast<uint4*>(r.dqkv + row * ld + 2 * r.C + col + e0) = Vec16<__nv_bfloat16>::from_float(acc2);
-    }
+  const float *bias = r.view.bias + (long long)h * r.view.pitch + r.view.center, *lse = r.lse + (long long)h * capacity;
+  const float* delta = r.delta + (long long)h * capacity;
+  float acc1[D / 2] = {}, acc2[D / 2] = {};  // dQ | dK and dV
+  for (int k = s.lo + lane; k < s.hi; k += 32) {
+    const int q = keys ? k : row, j = keys ? row : k;
+    const __nv_bfloat16 *Q = r.qkv + q * ld + col, *K = r.qkv + j * ld + r.C + col, *dO = r.dao + (long long)q * r.C + col;
+    const float l = lse[q], dp = rel_dot<D>(dO, K + r.C);
+    const float p = l == -CUDART_INF_F ? 0.f : exp2f(fmaf(rel_dot<D>(Q, K), r.scale * kLog2e, bias[r.view.pos[q] - r.view.pos[j]]) - l * kLog2e);
+    rel_axpy<D / 2>(acc1, p * (dp - delta[q]), (keys ? Q : K) + e0);
+    if (keys) rel_axpy<D / 2>(acc2, p, dO + e0);
   }
+  __nv_bfloat16* to = r.dqkv + row * ld + col + e0;
+  rel_store_sums<D / 2>(acc1, r.scale, to + (keys ? r.C : 0));
+  if (keys) rel_store_sums<D / 2>(acc2, 1.f, to + 2 * r.C);
 }
 
 // Sums by offset to the buckets' (see rel_few_buckets).  Neighbouring offsets are mostly of one bucket: a warp adds such up first.
@@ -186,9 +170,9 @@ __global__ void __launch_bounds__(256) rel_fold_kernel(const unsigned long long*
   }
 }
 
-// dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.  kRedo: behind
-// the tensor-core kernels, the rows that they noted down.
-template <bool kRedo>
+// dtable = acc / scale, NaN for a head with values that are not finite.  A token with two rows: an error in d_status.  D: behind
+// the tensor-core kernels, heads of D, the rows that they noted down; 0: no such rows.
+template <int D>
 __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const unsigned long long* acc, int n_buckets, const Redo r, const int32_t* seg, int n_seg, int capacity,
                                                          const int32_t* idx, const int32_t* owner, int tokens,
                                                          float* __restrict__ dtable, int32_t* d_status) {
@@ -211,9 +195,9 @@ __global__ void __launch_bounds__(256) rel_finish_kernel(const RelGrad g, const 
     const int t = ld_dep(idx + i);
     if ((unsigned)t < (unsigned)tokens && ld_dep(owner + t) != i) record_status(d_status, SPA_ERR_INVALID_ARG);
   }
-  if constexpr (kRedo) {
+  if constexpr (D != 0) {
     const uint32_t noted = (uint32_t)ld_dep(reinterpret_cast<const int32_t*>(g.redo)), n = noted < g.most_redo ? noted : g.most_redo;
-    for (uint32_t i = blockIdx.x * 8 + warp; i < n; i += gridDim.x * 8) redo_row(r, seg, n_seg, capacity, Np, g.redo[1 + i]);
+    for (uint32_t i = blockIdx.x * 8 + warp; i < n; i += gridDim.x * 8) redo_row<D>(r, seg, n_seg, capacity, Np, g.redo[1 + i]);
   }
 }
 
@@ -353,8 +337,8 @@ int launch_attention_rel_bwd(const spa_params& p, const spa_rel_bias& r, const v
   // behind the tensor-core kernels a CTA per SM, should there be rows to form again
   const int grid = (int)(!tc && (work + 1023) / 1024 < kNumSMs ? (work + 1023) / 1024 : kNumSMs);
   const Redo redo{view(l, ws), (const __nv_bfloat16*)qkv, (const __nv_bfloat16*)dao, lse, (const float*)(ws + l.delta), (__nv_bfloat16*)dqkv,
-               p.C, p.C / p.H, softmax_scale_of(p)};
-  launch_pdl(tc ? rel_finish_kernel<true> : rel_finish_kernel<false>, grid, 256, (size_t)p.H * sizeof(float), st, g, acc, r.n_buckets, redo, seg, n_seg, p.capacity,
+                  p.C, softmax_scale_of(p)};
+  launch_pdl(!tc ? rel_finish_kernel<0> : p.C / p.H == 64 ? rel_finish_kernel<64> : rel_finish_kernel<32>, grid, 256, (size_t)p.H * sizeof(float), st, g, acc, r.n_buckets, redo, seg, n_seg, p.capacity,
              idx, (const int32_t*)(ws + l.owner), p.B * p.N, dtable, d_status);
   SPA_CUDA_CHECK_LAUNCH("rel_finish_kernel");
   return SPA_OK;

@@ -10,6 +10,7 @@
 //   |dS_ij| = P_ij |dO_i . v_j - D_i| <= 2 P_ij |dO_i| max_j |v_j|     (O_i is a mean of the v_j)
 #pragma once
 
+#include "simt_stage.cuh"
 #include "sm100_ptx.cuh"
 #include "spa_common.cuh"
 
@@ -46,9 +47,53 @@ __device__ __forceinline__ int rel_position(int t, int before, int i, int N, int
   return n / cols * (2 * cols - 1) + n % cols;
 }
 
+// kN values from a 16-byte boundary on, all of them NaN.  A row that its own values have made NaN has nothing to be formed again: a call whose
+// inputs are NaN everywhere (after a step that diverged) formed every row so, 18 images of 24 x 24 with 77 to 576 rows, 4 heads of 64, 0.09 -> 557 ms.
+template <int kN> __device__ __forceinline__ bool rel_all_nan(const __nv_bfloat16* v) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v);  // a bf16 is NaN where its bits without the sign are above those of infinity
+#pragma unroll 1
+  for (int i = 0; i < kN / 2; ++i)
+    if ((w[i] & 0x7fffu) <= 0x7f80u || (w[i] >> 16 & 0x7fffu) <= 0x7f80u) return false;
+  return true;
+}
+// sum of a_e b_e over D values each from a 16-byte boundary on (a loop: what is formed again leaves the registers to the kernel around it)
+template <int D> __device__ __forceinline__ float rel_dot(const __nv_bfloat16* a, const __nv_bfloat16* b) {
+  float sum = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < D / 8; ++c) {
+    float f[8], g[8];
+    Vec16<__nv_bfloat16>::to_float(reinterpret_cast<const uint4*>(a)[c], f);
+    Vec16<__nv_bfloat16>::to_float(reinterpret_cast<const uint4*>(b)[c], g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(f[e], g[e], sum);
+  }
+  return sum;
+}
+// acc_e += w v_e
+template <int kN> __device__ __forceinline__ void rel_axpy(float (&acc)[kN], float w, const __nv_bfloat16* v) {
+#pragma unroll
+  for (int c = 0; c < kN / 8; ++c) {
+    float f[8];
+    Vec16<__nv_bfloat16>::to_float(reinterpret_cast<const uint4*>(v)[c], f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[8 * c + e] = fmaf(w, f[e], acc[8 * c + e]);
+  }
+}
+// The lanes' sums, times mul, as kN values from a 16-byte boundary on
+template <int kN> __device__ __forceinline__ void rel_store_sums(float (&acc)[kN], float mul, __nv_bfloat16* to) {
+#pragma unroll
+  for (int e = 0; e < kN; ++e) acc[e] = warp_sum(acc[e]) * mul;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int c = 0; c < kN / 8; ++c) reinterpret_cast<uint4*>(to)[c] = Vec16<__nv_bfloat16>::from_float(acc + 8 * c);
+}
+
 // A half of a row of the forward's output that is not finite: {row, head, half}, and the CTA's entry before it (numbers from 1 on; 0:
 // none), of which `last` in shared memory is the last.  The CTA that notes it down forms it again.
-__device__ __forceinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int capacity, int row, int h, int half) {
+// v: the row's own half of V.  A call, not in line: with the loads in the kernel around it 8 frames of 47 x 83 took 88 us instead of 83.
+template <int D>
+__device__ __noinline__ void rel_fwd_note(uint32_t* redo, uint32_t* last, int capacity, int row, int h, int half, const __nv_bfloat16* v) {
+  if (rel_all_nan<D / 2>(v)) return;
   const uint32_t at = 2u * ((uint32_t)h * capacity + row) + half + 1u;
   redo[2 * at - 1] = (uint32_t)row | (uint32_t)h << 20 | (uint32_t)half << 28;
   redo[2 * at] = atomicExch(last, at);
@@ -69,11 +114,33 @@ struct RelGrad {
   uint32_t most_redo;       // 4 H capacity
 };
 
-// A zero weight times an infinity or NaN of another segment in the same tile is NaN.  Halves of rows of dQ (keys = false) or of dK
-// and dV that are not finite are noted down, and formed again behind the attention from their own segment's rows alone.
+// A zero weight times an infinity or NaN of another segment in the same tile is NaN.  Halves of rows of dQ (keys = false), or of dK and dV, that
+// are not finite are noted down, and formed again behind the attention from their own segment's rows alone.
 __device__ __forceinline__ void rel_redo(const RelGrad& g, bool keys, int half, int h, int row) {
   const uint32_t at = atomicAdd(g.redo, 1u);
   if (at < g.most_redo) g.redo[1 + at] = (uint32_t)row | (uint32_t)h << 20 | (keys ? 1u : 0u) << 28 | (uint32_t)half << 29;
+}
+// The same where segments may be long, but for what its own values have made NaN: dQ by its row's logarithm of the sum (lse) or D (delta), of which one
+// makes every dS of the row NaN; dK and dV by those of the token's own row among the queries: lse makes P and dS NaN, D dS, so dK, and where
+// its half of a row of dO (own_do) is NaN, dV is.  bad: kBadQ, kBadK, kBadV.  A call, not in line, as rel_fwd_note is.  (Segments of up to 128
+// rows are formed again in no time: 64 of 7 x 7, 6 heads of 64, NaN everywhere, the backward takes as long as with numbers.)
+constexpr uint32_t kBadQ = 1, kBadK = 2, kBadV = 4;
+template <int D>
+__device__ __noinline__ void rel_note(uint32_t* redo, uint32_t most, uint32_t row, uint32_t h, uint32_t half, uint32_t bad, float lse, float delta,
+                                      const __nv_bfloat16* own_do) {
+  if (lse != lse) return;
+  if (delta != delta) bad &= kBadV;
+  auto note = [&](uint32_t keys) {
+    const uint32_t at = atomicAdd(redo, 1u);
+    if (at < most) redo[1 + at] = row | h << 20 | keys << 28 | half << 29;
+  };
+  if (bad & kBadQ) note(0u);
+  if ((bad & kBadK) || ((bad & kBadV) && !rel_all_nan<D / 2>(own_do))) note(1u);
+}
+template <int D>
+__device__ __forceinline__ void rel_redo_long(const RelGrad& g, uint32_t bad, int half, int h, int row, float lse, float delta,
+                                              const __nv_bfloat16* dao, int C) {
+  rel_note<D>(g.redo, g.most_redo, (uint32_t)row, (uint32_t)h, (uint32_t)half, bad, lse, delta, dao + (long long)row * C + h * D + half * (D / 2));
 }
 
 // Bits of the head's bound in the sums: as many as 64 hold.  The pairs of a query in a bin have dS of no more than the bound together (their P sum

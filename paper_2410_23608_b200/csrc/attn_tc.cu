@@ -106,43 +106,28 @@ template <int kRel> __device__ __forceinline__ int position_of(const RelView& re
 }
 
 // The rows that this CTA has noted down (see rel_fwd_note), from entry `at` on: a half of a row's output from the keys of its segment
-// alone, by a warp, the keys to its lanes.  table: the CTA's head's.
-template <int kRel>
-__device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, const int32_t* seg, int n_seg, int Np, int C, int d,
-                                           float scale_log2e, const RelView rel, const RelRaw raw, const float* table, uint32_t at) {
+// alone, by a warp, the keys to its lanes, whose weights follow from the row's logarithm of the sum.  table: the CTA's head's.
+template <int D, int kRel>
+__device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat16* ao, const float* lse, const int32_t* seg, int n_seg, int capacity,
+                                           int Np, int C, float scale_log2e, const RelView rel, const RelRaw raw, const float* table, uint32_t at) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = 0; at != 0u; ++i) {
     const uint32_t what = rel.redo[2 * at - 1];
     at = rel.redo[2 * at];
     if (i % (kFwdThreads / 32) != warp) continue;
-    const int row = what & 0xfffff, h = (what >> 20) & 0xff, first = ((what >> 28) & 1) * (d / 2);
+    const int row = what & 0xfffff, h = (what >> 20) & 0xff, e0 = h * D + ((what >> 28) & 1) * (D / 2);
     const RowSeg s = row_segment(seg, n_seg, Np, row);
-    const __nv_bfloat16* q = qkv + (long long)row * 3 * C + h * d;
+    const __nv_bfloat16* q = qkv + (long long)row * 3 * C + h * D;
     const float* bias = table + rel.center + position_of<kRel>(rel, raw, Np, row);
-    auto logit = [&](int j) {
-      const __nv_bfloat16* k = qkv + (long long)j * 3 * C + C + h * d;
-      float v = 0.f;
-      for (int e = 0; e < d; ++e) v = fmaf(__bfloat162float(q[e]), __bfloat162float(k[e]), v);
-      return fmaf(v, scale_log2e, bias[-position_of<kRel>(rel, raw, Np, j)]);
-    };
-    float m = -CUDART_INF_F;
-    for (int j = s.lo + lane; j < s.hi; j += 32) m = fmaxf(m, logit(j));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (m == -CUDART_INF_F) m = 0.f;
-    for (int e0 = first; e0 < first + d / 2; e0 += 8) {
-      float acc[8] = {}, l = 0.f;
+    const float l = lse[(long long)h * capacity + row] * 1.4426950408889634f;
+    for (int e = e0; e < e0 + D / 2; e += 16) {
+      float acc[16] = {};
       for (int j = s.lo + lane; j < s.hi; j += 32) {
-        const float p = ptx::ex2_approx(logit(j) - m);
-        const __nv_bfloat16* v = qkv + (long long)j * 3 * C + 2 * C + h * d + e0;
-        l += p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, __bfloat162float(v[e]), acc[e]);
+        const __nv_bfloat16* key = qkv + (long long)j * 3 * C + C;
+        const float p = ptx::ex2_approx(fmaf(rel_dot<D>(q, key + h * D), scale_log2e, bias[-position_of<kRel>(rel, raw, Np, j)]) - l);
+        rel_axpy<16>(acc, p, key + C + e);
       }
-      l = warp_sum(l);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = warp_sum(acc[e]) / l;
-      if (lane == 0) *reinterpret_cast<uint4*>(ao + (long long)row * C + h * d + e0) = Vec16<__nv_bfloat16>::from_float(acc);
+      rel_store_sums<16>(acc, 1.f, ao + (long long)row * C + e);
     }
   }
 }
@@ -703,7 +688,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
           if (keyless) r[e] = 0u;
           sum += fabsf(__uint_as_float(r[e]));
         }
-        again = !(sum < CUDART_INF_F) && rl < rows;
+        again = !(sum < CUDART_INF_F) && rl < rows && l_row == l_row;  // a row whose sum is NaN is so by itself
       }
       uint4 o16[kDh / 8];
 #pragma unroll
@@ -725,7 +710,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
       }
       if constexpr (kRel != kNoRel) {
         // A zero weight times an infinity or NaN of another segment of the tile is NaN: such rows again, at the end
-        if (again) rel_fwd_note(rel.redo, reinterpret_cast<uint32_t*>(smem_al + SM::kBar + 216), capacity, row, h, half);
+        if (again)
+          rel_fwd_note<D>(rel.redo, reinterpret_cast<uint32_t*>(smem_al + SM::kBar + 216), capacity, row, h, half,
+                          qkv + (long long)row * 3 * C + 2 * C + h * D + half * kDh);
       }
       if (half == 0 && rl < rows) {
         lse[(long long)h * capacity + row] = (m + log2f(l_row)) * 0.6931471805599453f;
@@ -744,7 +731,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm, const int32_t* seg, i
   if constexpr (kRel != kNoRel) {
     const uint32_t at = (uint32_t)ptx::lds_s32(redo_first);
     const float* table = in_shared(kRel) ? reinterpret_cast<const float*>(smem_al + SM::kTable) : rel.bias + (long long)((int)blockIdx.x % H) * rel.pitch;
-    if (at != 0u) rel_fwd_again<kRel>(qkv, ao, seg, n_seg, Np, C, D, scale_log2e, rel, raw, table, at);
+    if (at != 0u) rel_fwd_again<D, kRel>(qkv, ao, lse, seg, n_seg, capacity, Np, C, scale_log2e, rel, raw, table, at);
   }
 }
 
@@ -802,7 +789,7 @@ __device__ __forceinline__ int cluster_ctas() {
 template <int D, int kAcc>
 __device__ void split_join(uint8_t* smem_al, uint32_t tmem_at, const uint32_t (&acc_col)[kAcc], bool is_math, bool there, int rl, int half,
                            const volatile uint8_t* row_ok, __nv_bfloat16* dqkv, const int (&col)[kAcc], const float (&mul)[kAcc], int C, int r0, int h,
-                           const RelGrad& grad, bool keys) {
+                           const RelGrad& grad, const float* lse, const float* delta, const __nv_bfloat16* dao, int capacity) {
   constexpr int kDh = D / 2, kRow = D * 4, kSize = 128 * kRow;
   const int tid = threadIdx.x, lane = tid & 31;
   if (is_math) {
@@ -828,10 +815,11 @@ __device__ void split_join(uint8_t* smem_al, uint32_t tmem_at, const uint32_t (&
   for (int e = tid; e < share * (D / 8); e += kBwdThreads) {  // whole warps
     const int r = first + e / (D / 8), c = e % (D / 8);
     uint4 out[kAcc];
-    float sum = 0.f;
+    uint32_t bad = 0u;  // of a half of a row, in its first lane: see rel_redo
+    constexpr int kLanes = D / 16;
 #pragma unroll
     for (int a = 0; a < kAcc; ++a) {
-      float v[8];
+      float v[8], sum = 0.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         const float4 f = sum_dsmem4(reinterpret_cast<const float*>(smem_al + a * kSize + r * kRow + (((2 * c + g) ^ (r & 7)) << 4)), parts);
@@ -843,25 +831,27 @@ __device__ void split_join(uint8_t* smem_al, uint32_t tmem_at, const uint32_t (&
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += fabsf(v[i]);
       out[a] = Vec16<__nv_bfloat16>::from_float(v);
+      const bool in_half = ((__ballot_sync(0xffffffffu, !(sum < CUDART_INF_F)) >> lane) & ((1u << kLanes) - 1u)) != 0u;
+      if (in_half) bad |= kAcc == 1 ? kBadQ : a == 0 ? kBadV : kBadK;
     }
-    // a half of a row that is not finite: see rel_redo
-    constexpr int kLanes = D / 16;
-    const unsigned bad = __ballot_sync(0xffffffffu, !(sum < CUDART_INF_F));
     if (row_ok[r]) {
 #pragma unroll
       for (int a = 0; a < kAcc; ++a) *reinterpret_cast<uint4*>(dqkv + (long long)(r0 + r) * 3 * C + col[a] + c * 8) = out[a];
-      if (c % kLanes == 0 && ((bad >> lane) & ((1u << kLanes) - 1u)) != 0u) rel_redo(grad, keys, c / kLanes, h, r0 + r);
+      if (c % kLanes == 0 && bad != 0u)
+        rel_redo_long<D>(grad, bad, c / kLanes, h, r0 + r, lse[(long long)h * capacity + r0 + r], delta[(long long)h * capacity + r0 + r], dao, C);
     }
   }
 }
 
+// rel is read where it is used: of a copy (without __grid_constant__) parts stayed in registers, and the pass with a bias spilled twice as much (8 images
+// of 40 x 60 with 20 to 90 % selected, 8 heads of 64, backward 453 -> 501 us).  The kernels of attn_rel_short.cu spill less with the copy.
 template <int D, bool kDQ, bool kLoop, int kRel, bool kSplit = false>
 __global__ void __launch_bounds__(kBwdThreads, 2)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
                    const __grid_constant__ CUtensorMap tm_o,
                    const float* lse, float* delta, const int32_t* seg, int n_seg,
-                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const RelBwd rel, int32_t* d_status) {
+                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const __grid_constant__ RelBwd rel, const __nv_bfloat16* dao, int32_t* d_status) {
   using HT = HeadTile<D>;
   constexpr int kTile = HT::kTileBytes;             // own tiles: 128 rows
   constexpr int kYTile = kBwdY * HT::kRowBytes;     // streamed tiles: 64 rows
@@ -1421,8 +1411,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
-    bool again = false;
-    auto stage_acc = [&](uint32_t acc_col, uint8_t* tile, float mul) {
+    uint32_t bad = 0u;  // which of this thread's halves of rows are not finite
+    auto stage_acc = [&](uint32_t what, uint32_t acc_col, uint8_t* tile, float mul) {
       uint32_t r[kDh];
       if (kDh == 32) ptx::tmem_ld_32x32(tmem + lane_base + acc_col + half * kDh, r);
       else ptx::tmem_ld_32x16(tmem + lane_base + acc_col + half * kDh, r);
@@ -1432,7 +1422,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
-        again = again || !(sum < CUDART_INF_F);
+        if (!(sum < CUDART_INF_F)) bad |= what;
       }
 #pragma unroll
       for (int g = 0; g < kDh / 8; ++g) {
@@ -1445,19 +1435,20 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     };
     const long long ld = 3LL * C;
     if (kDQ) {
-      if (is_math) stage_acc(kColAcc1, smem_al, scale);
+      if (is_math) stage_acc(kBadQ, kColAcc1, smem_al, scale);
       __syncthreads();
       copy_tile_out<D, kBwdThreads>(smem_al, dqkv + h * D, ld, r0, Np, tid, row_ok);
     } else {
       if (is_math) {
-        stage_acc(kColAcc1, smem_al, 1.f);             // dV
-        stage_acc(kColAcc2, smem_al + kTile, scale);   // dK
+        stage_acc(kBadV, kColAcc1, smem_al, 1.f);             // dV
+        stage_acc(kBadK, kColAcc2, smem_al + kTile, scale);   // dK
       }
       __syncthreads();
       copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
       copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
     }
-    if (kRel != kNoRel && again && mine.hi > mine.lo) rel_redo(rel.grad, !kDQ, half, h, row);
+    if (kRel != kNoRel && bad != 0u && mine.hi > mine.lo)
+      rel_redo_long<D>(rel.grad, bad, half, h, row, lse[(long long)h * capacity + row], delta[(long long)h * capacity + row], dao, C);
   }
   if (kRel != kNoRel && kDQ && !failed && n_tiles > 0 && rel.shared_bins)  // the item's bins to the head's sums
     rel_flush<kBwdThreads>(rel, reinterpret_cast<const int*>(bins), h, range[0], tid);
@@ -1470,10 +1461,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
     __syncthreads();  // the tiles' memory is free
     const uint32_t at = tmem + lane_base + half * (D / 2);
     if constexpr (kDQ)
-      split_join<D, 1>(smem_al, at, {kColAcc1}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv, {h * D}, {scale}, C, r0, h, rel.grad, false);
+      split_join<D, 1>(smem_al, at, {kColAcc1}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv, {h * D}, {scale}, C, r0, h, rel.grad, lse, delta,
+                       dao, capacity);
     else
       split_join<D, 2>(smem_al, at, {kColAcc1, kColAcc2}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv, {2 * C + h * D, C + h * D},
-                       {1.f, scale}, C, r0, h, rel.grad, true);
+                       {1.f, scale}, C, r0, h, rel.grad, lse, delta, dao, capacity);
     __syncwarp();
     cluster_sync_all();  // nobody leaves while its accumulators are still being read
   }
@@ -1507,7 +1499,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
                    const __grid_constant__ CUtensorMap tm_qkv_y, const __grid_constant__ CUtensorMap tm_do_y,
                    const __grid_constant__ CUtensorMap tm_o,
                    const float* lse, float* delta, const int32_t* seg, int n_seg,
-                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const RelBwd rel, int32_t* d_status) {
+                   int capacity, int C, int H, float scale, __nv_bfloat16* __restrict__ dqkv, int skip_short, const __grid_constant__ RelBwd rel, const __nv_bfloat16* dao, int32_t* d_status) {
   using HT = HeadTile<D>;
   constexpr int kTile = HT::kTileBytes;             // own tiles: 128 rows
   constexpr int kYTile = kBwdY * HT::kRowBytes;     // streamed tiles: 64 rows
@@ -1945,8 +1937,8 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     // Each thread drains d/2 columns of its row of the accumulators into the own tiles' shared memory (idle
     // now: every product has completed), from where whole rows go out as full lines.
     constexpr int kDh = D / 2;
-    bool again = false;
-    auto stage_acc = [&](uint32_t acc_col, uint8_t* tile, float mul) {
+    uint32_t bad = 0u;  // which of this thread's halves of rows are not finite
+    auto stage_acc = [&](uint32_t what, uint32_t acc_col, uint8_t* tile, float mul) {
       uint32_t r[kDh];
       if (kDh == 32) ptx::tmem_ld_32x32(tmem + lane_base + acc_col + half * kDh, r);
       else ptx::tmem_ld_32x16(tmem + lane_base + acc_col + half * kDh, r);
@@ -1956,7 +1948,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < kDh; ++e) sum += fabsf(__uint_as_float(r[e]));
-        again = again || !(sum < CUDART_INF_F);
+        if (!(sum < CUDART_INF_F)) bad |= what;
       }
 #pragma unroll
       for (int g = 0; g < kDh / 8; ++g) {
@@ -1969,13 +1961,14 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
     };
     const long long ld = 3LL * C;
     if (is_math) {
-      stage_acc(kColAcc1, smem_al, 1.f);             // dV
-      stage_acc(kColAcc2, smem_al + kTile, scale);   // dK
+      stage_acc(kBadV, kColAcc1, smem_al, 1.f);             // dV
+      stage_acc(kBadK, kColAcc2, smem_al + kTile, scale);   // dK
     }
     __syncthreads();
     copy_tile_out<D, kBwdThreads>(smem_al, dqkv + 2 * C + h * D, ld, r0, Np, tid, row_ok);
     copy_tile_out<D, kBwdThreads>(smem_al + kTile, dqkv + C + h * D, ld, r0, Np, tid, row_ok);
-    if (kRel != kNoRel && again && mine.hi > mine.lo) rel_redo(rel.grad, true, half, h, row);
+    if (kRel != kNoRel && bad != 0u && mine.hi > mine.lo)
+      rel_redo_long<D>(rel.grad, bad, half, h, row, lse[(long long)h * capacity + row], delta[(long long)h * capacity + row], dao, C);
   }
   if ((failed || n_tiles == 0) && tid == kBwdMath) {  // let outstanding loads land before shared memory is released
     for (int t = issued > kStages ? issued - kStages : 0; t < issued; ++t) ptx::mbar_wait(bar_y(stage_of(t)), use_of(t));
@@ -1984,7 +1977,7 @@ attn_bwd_kv_split_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __gri
   if constexpr (kSplit) {
     __syncthreads();  // the tiles' memory is free
     split_join<D, 2>(smem_al, tmem + lane_base + half * (D / 2), {kColAcc1, kColAcc2}, is_math, !failed && n_tiles > 0, rl, half, row_ok, dqkv,
-                     {2 * C + h * D, C + h * D}, {1.f, scale}, C, r0, h, rel.grad, true);
+                     {2 * C + h * D, C + h * D}, {1.f, scale}, C, r0, h, rel.grad, lse, delta, dao, capacity);
     __syncwarp();
     cluster_sync_all();  // nobody leaves while its accumulators are still being read
   }
@@ -2334,10 +2327,10 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
       });
       if (es == cudaSuccess)
         es = launch_cluster(sq, grid * dq_parts, dq_parts, dq_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg, n_seg, p.capacity, p.C,
-                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, d_status);
+                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, (const __nv_bfloat16*)dao, d_status);
       if (es == cudaSuccess)
         es = launch_cluster(skv, grid * kv_parts, kv_parts, kv_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg, n_seg, p.capacity, p.C,
-                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, d_status);
+                            p.H, scale, (__nv_bfloat16*)dqkv, (int)long_only, rel, (const __nv_bfloat16*)dao, d_status);
       if (es != cudaSuccess) { set_cuda_error(es, "attn_bwd_tc_kernel"); return SPA_ERR_CUDA; }
       SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dKV)");
       return SPA_OK;
@@ -2353,12 +2346,12 @@ int bwd_launch(const spa_params& p, const void* qkv, const void* ao, const float
     SPA_CUDA_CHECK_LAUNCH("attn_bwd_short_kernel");
   }
   launch_pdl(kq, grid, kBwdThreads, dq_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
-             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, d_status);
+             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, (const __nv_bfloat16*)dao, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dQ)");
   if (kRel == kNoRel && attention_bwd_kv_applies(p, n_seg))
     return launch_attention_bwd_kv(p, qkv, lse, delta, dao, seg, n_seg, dqkv, skip_short != 0, d_status, st);
   launch_pdl(kkv, grid, KV::kThreads, kv_smem, st, tm_qkv, tm_do, tm_qkv_y, tm_do_y, tm_o, lse, delta, seg,
-             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, d_status);
+             n_seg, p.capacity, p.C, p.H, scale, (__nv_bfloat16*)dqkv, skip_short, rel, (const __nv_bfloat16*)dao, d_status);
   SPA_CUDA_CHECK_LAUNCH("attn_bwd_tc_kernel(dKV)");
   return SPA_OK;
 }
