@@ -685,50 +685,94 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 }
 
 // The parameters' gradients from the CTAs' sums, added up in their order: 32 channels a block, blockIdx.x = 0; and with a gate per
-// image, blockIdx.x = 1 + image, its gradient from its lines.
+// image, per_block images for each further blockIdx.x, their gradients from their lines: a block to an image, or where they have few lines each, a warp
+// (a block to each of 32 images of 576 x 768: 3 us more).
 constexpr int kJoinLanes = 16;
+// A sum with what its additions round off (each is a fp32 number that the additions themselves give: Moller's and Knuth's two-sum): a chain of 148
+// lines in fp32 was off by six times the result's own rounding.
+struct ExactSum {
+  float sum = 0.f, rest = 0.f;
+  __device__ __forceinline__ void add(float x) {
+    const float s = sum + x, t = s - sum;
+    rest += (sum - (s - t)) + (x - t);
+    sum = s;
+  }
+  __device__ __forceinline__ double value() const { return fabsf(sum) < __uint_as_float(0x7f800000u) ? (double)sum + rest : (double)sum; }
+};
+// In the order that they are written in: the loads of a round first, whatever the lines' number (else the kernel waits for memory line by line: 1 us)
+__device__ __forceinline__ float ld_f32(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+// Lines l, l + lanes, ... of kS sums of C channels each, kAtOnce of them on their way together
+template <int kAtOnce, int kS>
+__device__ __forceinline__ void join_lines(ExactSum (&v)[kSums], const float* at, int l, int lanes, int lines, int C) {
+  const size_t step = (size_t)lanes * kS * C;
+  const float* last = at;
+  at += (size_t)l * kS * C;
+  for (; l < lines; l += kAtOnce * lanes) {
+    float f[kAtOnce][kS];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i, at += step)
+#pragma unroll
+      for (int k = 0; k < kS; ++k) f[i][k] = ld_f32((l + i * lanes < lines ? at : last) + (unsigned)(k * C));
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+      for (int k = 0; k < kS; ++k) v[k].add(l + i * lanes < lines ? f[i][k] : 0.f);
+  }
+}
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinLanes)
-sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int N, int rows_per_cta, int C, const T* scale, const T* g_post,
+sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int B, int N, int per_block, int rows_per_cta, int C, const T* scale, const T* g_post,
                      const T* b_post, float* __restrict__ dgate, float* __restrict__ dscale, float* __restrict__ dg_post,
                      float* __restrict__ db_post, float* __restrict__ dg_pre, float* __restrict__ db_pre) {
   pdl_entry();
-  __shared__ float s[kSums][kJoinLanes][33];
+  __shared__ float s[kSums][kJoinLanes][33], rest[kSums][kJoinLanes][33];
+  __shared__ double total[kSums][32];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.y * 32 + x;
-  const bool images = blockIdx.x > 0;
+  const bool images = blockIdx.x > 0, alone = images && per_block > 1;  // alone: a thread has an image's lines by itself
+  const int b = ((int)blockIdx.x - 1) * per_block + (alone ? y : 0);
+  if (alone && b >= B) return;  // (without a barrier behind it)
   // an image's lines: those of the CTAs whose rows it has a part of
-  const int b = blockIdx.x - 1, c0 = images ? (int)((long long)b * N / rows_per_cta) : 0;
-  const int lines = images ? (int)(((long long)b * N + N - 1) / rows_per_cta) - c0 + 1 : ctas, sums = images ? 2 : kSums;
+  const int c0 = images ? (int)((long long)b * N / rows_per_cta) : 0;
+  const int lines = images ? (int)(((long long)b * N + N - 1) / rows_per_cta) - c0 + 1 : ctas;
   const float* from = images ? part_gate + (size_t)(b + c0) * 2 * C : part;
-  float v[kSums] = {};
+  const float sc = scale != nullptr && c < C ? to_f32<T>(scale[c]) : 1.f, gp = g_post != nullptr && c < C ? to_f32<T>(g_post[c]) : 1.f;
+  const float bp = b_post != nullptr && c < C ? to_f32<T>(b_post[c]) : 0.f;
+  ExactSum v[kSums];
   if (c < C) {
-#pragma unroll 4
-    for (int l = y; l < lines; l += kJoinLanes) {
-#pragma unroll
-      for (int k = 0; k < kSums; ++k)
-        if (k < sums) v[k] += from[((size_t)l * sums + k) * C + c];
-    }
+    if (alone) join_lines<4, 2>(v, from + c, 0, 1, lines, C);
+    else if (images) join_lines<4, 2>(v, from + c, y, kJoinLanes, lines, C);
+    else join_lines<5, kSums>(v, from + c, y, kJoinLanes, lines, C);  // 148 lines are two rounds
   }
-#pragma unroll
-  for (int k = 0; k < kSums; ++k) s[k][y][x] = v[k];
-  __syncthreads();
-  if (y != 0 || c >= C) return;
-#pragma unroll
-  for (int k = 0; k < kSums; ++k) {
-    v[k] = 0.f;
-    for (int l = 0; l < kJoinLanes; ++l) v[k] += s[k][l][x];
-  }
-  const float sc = scale != nullptr ? to_f32<T>(scale[c]) : 1.f, gp = g_post != nullptr ? to_f32<T>(g_post[c]) : 1.f;
-  const float bp = b_post != nullptr ? to_f32<T>(b_post[c]) : 0.f;
-  if (images) {
-    dgate[(size_t)(blockIdx.x - 1) * C + c] = sc * fmaf(gp, v[0], bp * v[1]);
+  if (alone) {
+    if (c < C) dgate[(size_t)b * C + c] = (float)((double)sc * (gp * v[0].value() + bp * v[1].value()));
     return;
   }
-  if (dscale != nullptr) dscale[c] = fmaf(gp, v[0], bp * v[1]);
-  if (dg_post != nullptr) dg_post[c] = sc * v[0];
-  if (db_post != nullptr) db_post[c] = sc * v[1];
-  if (dg_pre != nullptr) dg_pre[c] = v[2];
-  if (db_pre != nullptr) db_pre[c] = v[3];
+#pragma unroll
+  for (int k = 0; k < kSums; ++k) { s[k][y][x] = v[k].sum; rest[k][y][x] = v[k].rest; }
+  __syncthreads();
+  if (y < kSums) {  // a warp to a sum
+    ExactSum& u = v[0];
+    u = ExactSum{s[y][0][x], rest[y][0][x]};
+#pragma unroll
+    for (int l = 1; l < kJoinLanes; ++l) { u.add(s[y][l][x]); u.rest += rest[y][l][x]; }
+    total[y][x] = u.value();
+  }
+  __syncthreads();
+  if (y != 0 || c >= C) return;
+  const double t[kSums] = {total[0][x], total[1][x], total[2][x], total[3][x]};
+  if (images) {
+    dgate[(size_t)b * C + c] = (float)((double)sc * (gp * t[0] + bp * t[1]));
+    return;
+  }
+  if (dscale != nullptr) dscale[c] = (float)(gp * t[0] + bp * t[1]);
+  if (dg_post != nullptr) dg_post[c] = (float)(sc * t[0]);
+  if (db_post != nullptr) db_post[c] = (float)(sc * t[1]);
+  if (dg_pre != nullptr) dg_pre[c] = (float)t[2];
+  if (db_pre != nullptr) db_pre[c] = (float)t[3];
 }
 
 int chunks_of(const spa_params& p) { return p.C / (p.dtype == SPA_F32 ? 4 : 8); }
@@ -740,16 +784,21 @@ int warps_of(int Q) {
   return 16;
 }
 
-// The backward's shares of rows.  Images of one token: their gate is one per token, and no sum leaves a CTA for it.
+// The backward's shares of rows.  Images of one token: their gate is one per token, and no sum leaves a CTA for it.  A thread adds at most
+// kMostChain rows one after the other, and a CTA the sums of as many images: each addition is off by 2^-24 of the sum, and 2^20 rows of 4 096 had
+// chains of 7 085.  More CTAs then, in whole grids.
+constexpr int kMostChain = 256;
 struct Plan { int ctas, rows_per_cta, gate_kind; };
 Plan bwd_plan(const spa_params& p, const spa_sandwich& s) {
   const int groups = groups_of(warps_of(chunks_of(p)), true), rows = p.B * p.N;
+  Plan r;
+  r.gate_kind = s.gate_kind == SPA_GATE_IMAGE && p.N == 1 ? (int)SPA_GATE_TOKEN : s.gate_kind;
+  const int most = kMostChain * (r.gate_kind == SPA_GATE_IMAGE && p.N < groups ? p.N : groups);  // rows of a share
   int ctas = (rows + groups - 1) / groups;
   ctas = ctas < 1 ? 1 : (ctas > kNumSMs ? kNumSMs : ctas);
-  Plan r;
+  if ((rows + ctas - 1) / ctas > most) ctas = (rows + most * kNumSMs - 1) / (most * kNumSMs) * kNumSMs;
   r.rows_per_cta = rows > 0 ? (rows + ctas - 1) / ctas : 1;
   r.ctas = rows > 0 ? (rows + r.rows_per_cta - 1) / r.rows_per_cta : 1;
-  r.gate_kind = s.gate_kind == SPA_GATE_IMAGE && p.N == 1 ? (int)SPA_GATE_TOKEN : s.gate_kind;
   return r;
 }
 
@@ -869,9 +918,10 @@ int launch_sandwich_bwd(const spa_params& p, const spa_sandwich& s, const void* 
   if (rc != SPA_OK) return rc;
   const bool images = pl.gate_kind == SPA_GATE_IMAGE && dgate != nullptr;
   if (!images && dscale == nullptr && dg_post == nullptr && db_post == nullptr && dg_pre == nullptr && db_pre == nullptr) return SPA_OK;
-  const dim3 grid(images ? 1 + p.B : 1, (p.C + 31) / 32);
+  const int per_block = p.N / pl.rows_per_cta + 2 <= kJoinLanes ? kJoinLanes : 1;  // an image has at most so many lines
+  const dim3 grid(images ? 1 + (p.B + per_block - 1) / per_block : 1, (p.C + 31) / 32);
 #define SPA_JOIN(T)                                                                                                       \
-  launch_pdl(sandwich_join_kernel<T>, grid, 32 * kJoinLanes, 0, st, a.part, a.part_gate, pl.ctas, p.N, pl.rows_per_cta, p.C, \
+  launch_pdl(sandwich_join_kernel<T>, grid, 32 * kJoinLanes, 0, st, a.part, a.part_gate, pl.ctas, p.B, p.N, per_block, pl.rows_per_cta, p.C, \
              (const T*)s.scale, (const T*)s.g_post, (const T*)s.b_post, (float*)dgate, dscale, dg_post, db_post, dg_pre, db_pre)
   if (p.dtype == SPA_F32) SPA_JOIN(float); else SPA_JOIN(__nv_bfloat16);
 #undef SPA_JOIN
