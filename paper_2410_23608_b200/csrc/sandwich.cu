@@ -13,7 +13,8 @@
 // converted and every parameter read again in each of its three steps, 18 432 rows of 768 took 102 us against 26 for their
 // bytes.  So a row belongs to as many warps as leave a thread one 16-byte chunk (two beyond 512 chunks), arithmetic is on pairs of
 // fp32, products of parameters are held in registers, and the next row's loads are on their way under the arithmetic of
-// a row.  Statistics and sums are fp32; y and n are rounded once, n from the unrounded y.  Sums run in a fixed order: results
+// a row.  Statistics and sums are fp32; y and n are rounded once, n from the unrounded y.  Normalised values are (v - m) r: as v r - m r,
+// with m r rounded, they lost as many bits as the mean has deviations.  Sums run in a fixed order: results
 // are bitwise reproducible.
 #include "simt_stage.cuh"
 #include "sm100_ptx.cuh"
@@ -232,8 +233,8 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
 #pragma unroll
     for (int i = 0; i < P; ++i) { cw[k][i] = mul2(cw[k][i], sc[i]); cb[k][i] = mul2(cb[k][i], sc[i]); }
   }
-  // mean (0 for RMS) and 1 / deviation of the row v, whose chunks past the end are zero
-  auto statistics = [&](const uint64_t (&v)[kCh][P], float& mean, float& rstd) {
+  // mean (0 for RMS) and 1 / deviation of the row v, whose chunks past the end are zero; its chunks without the mean
+  auto statistics = [&](uint64_t (&v)[kCh][P], float& mean, float& rstd) {
     mean = 0.f;
     if (layer) {
       uint64_t s = 0ull;
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
     for (int k = 0; k < kCh; ++k)
       if (t0 + G * k < a.Q) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) { const uint64_t d = add2(v[k][i], m); ss = fma2(d, d, ss); }
+        for (int i = 0; i < P; ++i) { v[k][i] = add2(v[k][i], m); ss = fma2(v[k][i], v[k][i], ss); }
       }
     float t[1] = {sum_of(ss)};
     sum(t);
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
 #pragma unroll
       for (int k = 0; k < kCh; ++k) to_pairs(zv[k], v[k]);
       statistics(v, m1, r1);
-      const uint64_t r = both(r1), m = both(-m1 * r1), w = both(kGate == SPA_GATE_SCORE ? sigmoid(score) : 1.f);
+      const uint64_t r = both(r1), w = both(kGate == SPA_GATE_SCORE ? sigmoid(score) : 1.f);
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
         uint64_t x[P], g[P];
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
         if (kGateRows<kGate>) to_pairs(gr[k], g);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-          const uint64_t b = fma2(fma2(v[k][i], r, m), cw[k][i], cb[k][i]);
+          const uint64_t b = fma2(mul2(v[k][i], r), cw[k][i], cb[k][i]);
           v[k][i] = kGate == SPA_GATE_NONE ? add2(b, x[i]) : fma2(b, kGateRows<kGate> ? g[i] : w, x[i]);
         }
         if (t0 + G * k < a.Q) a.out_y[at + G * k] = from_pairs(v[k]);
@@ -342,12 +343,12 @@ __global__ void __launch_bounds__(threads_of(W, false), kCh == 1 ? 1024 / thread
     }
     if (a.out_n != nullptr) {
       statistics(v, m2, r2);
-      const uint64_t r = both(r2), m = both(-m2 * r2);
+      const uint64_t r = both(r2);
 #pragma unroll
       for (int k = 0; k < kCh; ++k) {
         if (t0 + G * k < a.Q) {
 #pragma unroll
-          for (int i = 0; i < P; ++i) v[k][i] = fma2(fma2(v[k][i], r, m), cp[k][i], bp[k][i]);
+          for (int i = 0; i < P; ++i) v[k][i] = fma2(mul2(v[k][i], r), cp[k][i], bp[k][i]);
           a.out_n[at + G * k] = from_pairs(v[k]);
         }
       }
@@ -545,7 +546,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
         float s[2 * R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const uint64_t rs = both(r2[r]), m = both(-m2[r] * r2[r]);
+          const uint64_t rs = both(r2[r]), m = both(-m2[r]);
           uint64_t s1 = 0ull, s2 = 0ull;
 #pragma unroll
           for (int k = 0; k < kCh; ++k) {
@@ -554,7 +555,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
             to_pairs(yr[r][k], yh[r][k]);
 #pragma unroll
             for (int i = 0; i < P; ++i) {  // chunks past the end: n is zero
-              yh[r][k][i] = fma2(yh[r][k][i], rs, m);
+              yh[r][k][i] = mul2(add2(yh[r][k][i], m), rs);
               sG[k][i] = fma2(n[i], yh[r][k][i], sG[k][i]);
               sN[k][i] = add2(sN[k][i], n[i]);
               d[r][k][i] = mul2(n[i], cp[k][i]);
@@ -591,7 +592,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         if (kGate == SPA_GATE_SCORE) score[r] = has[r] ? sigmoid(score[r]) : 0.f;  // without a row it may be NaN, or was not copied
-        const uint64_t rs = both(r1[r]), m = both(-m1[r] * r1[r]), w = both(score[r]);
+        const uint64_t rs = both(r1[r]), m = both(-m1[r]), w = both(score[r]);
         uint64_t u1 = 0ull, u2 = 0ull, u3 = 0ull;
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
@@ -603,7 +604,7 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 #pragma unroll
           for (int i = 0; i < P; ++i) {
             if (!in || !has[r]) d[r][k][i] = 0ull;  // past the end: the means' part; without a row: nothing
-            zh[r][k][i] = fma2(zh[r][k][i], rs, m);
+            zh[r][k][i] = mul2(add2(zh[r][k][i], m), rs);
             if (kGate == SPA_GATE_SCORE) u3 = fma2(d[r][k][i], fma2(zh[r][k][i], cw[k][i], cb[k][i]), u3);
             if constexpr (kGate == SPA_GATE_TOKEN) {
               const uint64_t dg = mul2(d[r][k][i], fma2(zh[r][k][i], cw[k][i], cb[k][i]));
