@@ -686,9 +686,9 @@ __global__ void __launch_bounds__(threads_of(W, true), 1) sandwich_bwd_kernel(co
 }
 
 // The parameters' gradients from the CTAs' sums, added up in their order: 32 channels a block, blockIdx.x = 0; and with a gate per
-// image, per_block images for each further blockIdx.x, their gradients from their lines: a block to an image, or where they have few lines each, a warp
-// (a block to each of 32 images of 576 x 768: 3 us more).
-constexpr int kJoinLanes = 16;
+// image, per_block images for each further blockIdx.x, their gradients from their lines: a block to an image, or where they have at most
+// kAloneLines each, a warp (a block to each of 32 images of 576 x 768: 3 us more; a warp to each of 16 of 196 x 384 fp32, ten lines: 1 us more).
+constexpr int kJoinLanes = 16, kAloneLines = 8;
 // A sum with what its additions round off (each is a fp32 number that the additions themselves give: Moller's and Knuth's two-sum): a chain of 148
 // lines in fp32 was off by six times the result's own rounding.
 struct ExactSum {
@@ -744,8 +744,8 @@ sandwich_join_kernel(const float* part, const float* part_gate, int ctas, int B,
   const float bp = b_post != nullptr && c < C ? to_f32<T>(b_post[c]) : 0.f;
   ExactSum v[kSums];
   if (c < C) {
-    if (alone) join_lines<4, 2>(v, from + c, 0, 1, lines, C);
-    else if (images) join_lines<4, 2>(v, from + c, y, kJoinLanes, lines, C);
+    if (alone) join_lines<kAloneLines, 2>(v, from + c, 0, 1, lines, C);
+    else if (images) join_lines<5, 2>(v, from + c, y, kJoinLanes, lines, C);
     else join_lines<5, kSums>(v, from + c, y, kJoinLanes, lines, C);  // 148 lines are two rounds
   }
   if (alone) {
@@ -919,7 +919,7 @@ int launch_sandwich_bwd(const spa_params& p, const spa_sandwich& s, const void* 
   if (rc != SPA_OK) return rc;
   const bool images = pl.gate_kind == SPA_GATE_IMAGE && dgate != nullptr;
   if (!images && dscale == nullptr && dg_post == nullptr && db_post == nullptr && dg_pre == nullptr && db_pre == nullptr) return SPA_OK;
-  const int per_block = p.N / pl.rows_per_cta + 2 <= kJoinLanes ? kJoinLanes : 1;  // an image has at most so many lines
+  const int per_block = p.N / pl.rows_per_cta + 2 <= kAloneLines ? kJoinLanes : 1;  // an image has at most so many lines
   const dim3 grid(images ? 1 + (p.B + per_block - 1) / per_block : 1, (p.C + 31) / 32);
 #define SPA_JOIN(T)                                                                                                       \
   launch_pdl(sandwich_join_kernel<T>, grid, 32 * kJoinLanes, 0, st, a.part, a.part_gate, pl.ctas, p.B, p.N, per_block, pl.rows_per_cta, p.C, \
