@@ -203,6 +203,8 @@ int spa_packed_attention_bwd_static(const spa_params* p, const void* qkv, const 
  *   bucket: int32[(2 rows - 1) * (2 cols - 1)], each in [0, n_buckets): a bucket for every offset, or few for many;
  *   table: T[n_buckets][H].  An entry of -inf, or below -1e6, masks its bucket; a row that is left without a key gives zeros,
  *   lse = -inf, peak = 0 and no gradient.
+ * bf16 on tensor cores: products and sums in fp32, but P is rounded to bf16 in front of the product with V, and in the backward P and dS
+ * in front of those that use them, each by 2^-8 at most, as in spa_packed_attention_fwd / _bwd; SPA_FLAG_SIMT_ONLY keeps them in fp32.
  * peak: float[H][capacity] out, the logarithm of the row's largest probability (max_j S_ij - lse_i), for the backward.
  * A segment must hold tokens of one image (images, or parts of them such as containers), and no token twice: the device records
  * SPA_ERR_INVALID_ARG in d_status where it does not, and for an idx or a bucket out of range (no access goes out of bounds; the
@@ -228,7 +230,7 @@ int spa_packed_attention_rel_fwd(const spa_params* p, const spa_rel_bias* rel, c
  * 2 |d_attn_out_i| |v|, the largest of the head; b = 62 - log2(capacity), rounded down, at least 42 and at most 46.  fp32 problems and
  * SPA_FLAG_SIMT_ONLY: each dS by 2^-b of the head's.  No norm of a row of V or d_attn_out counts as less than 2^-63.  Where a value of V, K or d_attn_out, the square of a row's norm, or a row's lse or D is
  * not finite, the whole head's column of dtable may be NaN.  dqkv has infinities and NaN of a segment in that segment's rows only
- * (rows whose tile they reach are formed again: such a call is slower).  SPA_FLAG_ONE_PASS_BWD has no effect. */
+ * (rows that another segment's may have reached are formed again: such a call is slower; one that is NaN everywhere is not).  SPA_FLAG_ONE_PASS_BWD has no effect. */
 int spa_packed_attention_rel_bwd(const spa_params* p, const spa_rel_bias* rel, const void* qkv, const void* attn_out, const float* lse,
                                  const float* peak, const void* d_attn_out, const int32_t* seg_offsets, int32_t n_seg,
                                  const int32_t* idx, void* dqkv, float* dtable, void* workspace, int32_t* d_status, void* stream);
@@ -389,7 +391,9 @@ int spa_sandwich_norm(const spa_params* p, const spa_sandwich* s, const void* x,
  * NULL.  y, z, z_row, stats: of the forward call (y may be NULL with dn).
  *   dx: T[B*N][C] out, may be dy; dz: like z, only rows that a token names are written;
  *   dgate: float[B*N] (SCORE), float[B][C] (IMAGE), T[B*N][C] (TOKEN) out; dscale, dg_post, db_post, dg_pre, db_pre: float[C] out.
- * dgate and each of the five may be NULL.  Sums run in a fixed order: results are bitwise reproducible.
+ * dgate and each of the five may be NULL.  Sums run in a fixed order: results are bitwise reproducible.  Of a sum over rows, at most 256 are
+ * added one after the other in fp32 (with a gate per image: and as many images), then up to 12 such sums; the rest is added with what the
+ * additions round off.
  * workspace: spa_sandwich_workspace_bytes() bytes. */
 size_t spa_sandwich_workspace_bytes(const spa_params* p, const spa_sandwich* s);
 int spa_sandwich_norm_bwd(const spa_params* p, const spa_sandwich* s, const void* dn, const void* dy, const void* y, const void* z,

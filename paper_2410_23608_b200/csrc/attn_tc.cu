@@ -143,7 +143,7 @@ __device__ __noinline__ void rel_fwd_again(const __nv_bfloat16* qkv, __nv_bfloat
 // kRel: S gets a bias by relative position, in units of log 2.  A tile's keys come as positions in shared memory; a pair's bias is
 // then one subtraction and one look-up in the head's table, in shared memory (kRelShared) or, where that is too small, in global
 // memory.  All items of a CTA are of one head, so that its table is fetched once; the row tiles of a head are drawn from a counter
-// of its own.  8 frames of 47 x 83 with 10 to 50 % selected, 8 heads of 32: 82 us, without a bias 55; issue slots 38 %, a warp waits 9 clocks from one
+// of its own.  8 frames of 47 x 83 with 10 to 50 % selected, 8 heads of 32: 83 us, without a bias 55; issue slots 39 %, a warp waits 9 clocks from one
 // instruction to its next.
 template <int D, int kRel>
 __global__ void __launch_bounds__(kFwdThreads, 2)
@@ -902,8 +902,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_cons
   // rows of this tile whose results this kernel writes (all valid rows, or those of the long segments only)
   volatile uint8_t* row_ok = reinterpret_cast<volatile uint8_t*>(smem_al + kBarBase + 128 + kSegStage * 4 + 64);
   // With a bias: positions of the streamed rows [3][64], the head's table (kRelShared), the item's bins (dQ pass, shared_bins).  32 images of
-  // 24 x 24 with 10 to 90 % selected, 12 heads of 64: this pass 104 us of 190, 34 % of the issue slots, and without its bins hardly less: the chain
-  // of a tile bounds it, which has twice the instructions of the one without a bias (15.8 a pair instead of 7.6).
+  // 24 x 24 with 10 to 90 % selected, 12 heads of 64: this pass 102 us of 189, 39 % of the issue slots: the chain of a tile bounds it, which
+  // has twice the instructions of the one without a bias (16.2 a pair instead of 7.6).
   constexpr int kPosBase = kBarBase + 128 + kSegStage * 4 + 64 + 128, kTableBase = kPosBase + kBwdPosBytes;
   const uint32_t pos_s = smem_base + kPosBase, table_s = smem_base + kTableBase;
   const uint32_t bins_s = table_s + (kRel == kRelShared ? rel.view.pitch * 4 : 0);
