@@ -73,6 +73,15 @@ def test_gates_of_another_type_or_size(lib, problem, kind, right, size):
                 call()
 
 
+def test_a_second_problem_is_looked_at_as_the_first(lib):
+    s = lib.sandwich("rms", "image", gate=torch.zeros(4, 64), scale=torch.zeros(64))
+    fit, wide, many = (lib.make_params(*a, 1, "f32") for a in ((4, 5, 64), (2, 5, 128), (5, 5, 64)))
+    for p, right in ((fit, True), (fit, True), (wide, False), (many, False), (fit, True), (lib.make_params(4, 5, 64, 1, "bf16"), False)):
+        for call in _sandwich_calls(lib, p, s):
+            with pytest.raises(lib.SpaError if right else ValueError):
+                call()
+
+
 def test_parameters_that_differ_among_themselves(lib):
     f, b = torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)
     for kw in (dict(scale=f, g_pre=b), dict(scale=f, g_pre=f[:32]), dict(scale=b, gate=f, gate_kind="image"), dict(b_pre=f.half()),
